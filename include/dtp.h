@@ -333,6 +333,120 @@ dtp_status dtp_apply_layout(const dtp_layer_desc* desc, int32_t L, const int32_t
                             const int32_t* nu, const void* const* src, void* const* dst,
                             void* stream);
 
+/* ---------------------------------------------------------------------------------------
+ * The dense decoder layer around the attention: what a calibration runs for x, attn and x_next,
+ * and what runs and trains a layer before and after its layout is applied.
+ *
+ * Shared by these entry points:
+ *   - Tensors are dense row-major in `dtype` unless said otherwise, every pointer 16-byte
+ *     aligned.  Any sizes > 0 are taken, up to 2^20 features, 2^31 weights and 2^30 tokens
+ *     (DTP_ERR_UNSUPPORTED beyond); multiples of 8 features need no padded copies.
+ *     n_tokens == 0 is a no-op, except that gradients of weights are then zeros.
+ *   - Sums are held in 32 bits or more and rounded to `dtype` once.  bf16 gradients of an
+ *     activation enter the products that follow rounded to bf16; nothing else is rounded on
+ *     the way.  Results are deterministic for fixed shapes.
+ *   - Outputs must not overlap inputs or each other, except where said (DTP_ERR_INVALID_ARG).
+ *   - `workspace` (dev, `workspace_bytes` long, or NULL) is scratch of at least the size that
+ *     the operator's _workspace function gives; it holds nothing between calls, and calls that
+ *     share it must be ordered (one stream, or synchronised; so must replays of graphs that
+ *     captured it).  With a workspace a call makes no allocation and can be captured into a
+ *     graph.  With NULL the scratch comes from the stream-ordered allocator, which is refused
+ *     under capture (DTP_ERR_UNSUPPORTED) where a call needs any.
+ * ------------------------------------------------------------------------------------- */
+
+/* Activations: none, silu(z) = z / (1 + e^-z), gelu(z) = z/2 (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))). */
+typedef enum { DTP_ACT_NONE = 0, DTP_ACT_SILU = 1, DTP_ACT_GELU = 2 } dtp_activation;
+
+/* Bytes of workspace of dtp_linear_forward and, with `backward`, of dtp_linear_backward too;
+ * -1 for arguments that those refuse. */
+int64_t dtp_linear_workspace(int64_t n_tokens, int32_t n_in, int32_t n_out, dtp_dtype dtype,
+                             dtp_activation act, int32_t backward);
+
+/* Matrix product with bias, activation and residual:
+ *   z = x W^T + b,  y = residual + alpha act(z).
+ *   x [n_tokens, n_in], w [n_out, n_in], bias [n_out] or NULL
+ *   residual [n_tokens, n_out] or NULL (none is added); y [n_tokens, n_out], may be `residual`
+ *   alpha   finite; sqrt(L) scales a device's own partial sum (Section 3, eqs. "stage1"-"stage3")
+ *   pre     [n_tokens, n_out] float or NULL: z, kept for the backward pass */
+dtp_status dtp_linear_forward(int64_t n_tokens, int32_t n_in, int32_t n_out, dtp_dtype dtype,
+                              const void* x, const void* w, const void* bias, const void* residual,
+                              dtp_activation act, float alpha, void* y, float* pre, void* workspace,
+                              int64_t workspace_bytes, void* stream);
+
+/* Its gradients, given dy [n_tokens, n_out] (which is also the residual's):
+ *   dz = alpha act'(z) dy,  dx = dz W,  dw = dz^T x,  dbias = sum_t dz.
+ *   pre    z as the forward call kept it; unused (may be NULL) without an activation
+ *   dx [n_tokens, n_in], dw [n_out, n_in], dbias [n_out]: written; NULL leaves one out
+ *   x is unused without dw, w without dx (NULL is accepted then) */
+dtp_status dtp_linear_backward(int64_t n_tokens, int32_t n_in, int32_t n_out, dtp_dtype dtype,
+                               const void* x, const void* w, const void* dy, dtp_activation act,
+                               float alpha, const float* pre, void* dx, void* dw, void* dbias,
+                               void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Bytes of workspace of dtp_gated_forward and, with `backward`, of dtp_gated_backward too;
+ * -1 for arguments that those refuse. */
+int64_t dtp_gated_workspace(int64_t n_tokens, int32_t d_model, int32_t n_neurons, dtp_dtype dtype,
+                            int32_t backward);
+
+/* Gated feed-forward block up to its down projection (which is dtp_linear_forward's):
+ *   g = x W_gate^T, u = x W_up^T, h = act(g) u,
+ * both projections, the activation and the product in one kernel.  With DTP_ACT_SILU g and u are
+ * the operating point of the affinity scores and h the neurons' alpha_k.
+ *   x [n_tokens, d]  the normed input; w_gate, w_up [I, d]; h [n_tokens, I]
+ *   act  DTP_ACT_SILU or DTP_ACT_GELU
+ *   pre  [n_tokens, 2, I] float or NULL: a token's g, then its u, kept for the backward pass */
+dtp_status dtp_gated_forward(int64_t n_tokens, int32_t d_model, int32_t n_neurons, dtp_dtype dtype,
+                             const void* x, const void* w_gate, const void* w_up, dtp_activation act,
+                             void* h, float* pre, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Its gradients, given dh [n_tokens, I] and pre as the forward call kept it:
+ *   dg = dh u act'(g), du = dh act(g),
+ *   dx = dg W_gate + du W_up, dw_gate = dg^T x, dw_up = du^T x.
+ *   dx [n_tokens, d], dw_gate and dw_up [I, d]: written; dx NULL, or both dw NULL, leaves those out
+ *   x is unused without the dw, w_gate and w_up without dx (NULL is accepted then) */
+dtp_status dtp_gated_backward(int64_t n_tokens, int32_t d_model, int32_t n_neurons, dtp_dtype dtype,
+                              const void* x, const void* w_gate, const void* w_up, dtp_activation act,
+                              const float* pre, const void* dh, void* dx, void* dw_gate, void* dw_up,
+                              void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Bytes of workspace of dtp_qk_norm_rotate_backward; -1 for arguments that it refuses. */
+int64_t dtp_qk_norm_rotate_workspace(int64_t n_tokens, int32_t n_q_heads, int32_t n_kv_groups,
+                                     int32_t head_dim, dtp_dtype dtype);
+
+/* Norms of queries and keys for each head, and their rotation by position, in one pass:
+ *   n = gamma * v / sqrt(mean(v^2) + eps)         for each head v of q (gamma_q) and k (gamma_k)
+ *   out_j       = n_j cos a_j - n_{j+R/2} sin a_j
+ *   out_{j+R/2} = n_{j+R/2} cos a_j + n_j sin a_j   for j < R/2, a_j = position * inv_freq_j,
+ *   the columns from R on as they are.
+ *   q [n_tokens, H, dh] and k [n_tokens, G, dh], whose tokens are q_stride and k_stride elements
+ *     apart (H * dh and G * dh where dense): slices of a packed projection are taken as they
+ *     are, at any address (16-byte alignment of every head makes the widest loads)
+ *   q_out [n_tokens, H, dh], k_out [n_tokens, G, dh] dense; may be q and k where those are dense
+ *   gamma_q, gamma_k [dh], or both NULL: no norm
+ *   positions [n_tokens] int32 and inv_freq [R/2] float, or both NULL with rot_dim R = 0: no
+ *     rotation.  Angles are formed in 64 bits, so positions may be far, and of either sign.
+ * head_dim even, 2 to 256; R even, at most head_dim; a norm, a rotation or both. */
+dtp_status dtp_qk_norm_rotate_forward(int64_t n_tokens, int32_t n_q_heads, int32_t n_kv_groups,
+                                      int32_t head_dim, dtp_dtype dtype, const void* q, int64_t q_stride,
+                                      const void* k, int64_t k_stride, const void* gamma_q,
+                                      const void* gamma_k, float eps, const int32_t* positions,
+                                      const float* inv_freq, int32_t rot_dim, void* q_out, void* k_out,
+                                      void* stream);
+
+/* Its gradients, from the forward call's inputs (which it must not have overwritten):
+ *   dq_out [n_tokens, H, dh], dk_out [n_tokens, G, dh]  dense, the gradients of its outputs
+ *   dq [n_tokens, H, dh], dk [n_tokens, G, dh]  dense, written; may be dq_out and dk_out
+ *   dgamma_q, dgamma_k [dh]  summed over tokens and heads, written; both NULL where there is no
+ *     norm, or to leave them out */
+dtp_status dtp_qk_norm_rotate_backward(int64_t n_tokens, int32_t n_q_heads, int32_t n_kv_groups,
+                                       int32_t head_dim, dtp_dtype dtype, const void* q, int64_t q_stride,
+                                       const void* k, int64_t k_stride, const void* gamma_q,
+                                       const void* gamma_k, float eps, const int32_t* positions,
+                                       const float* inv_freq, int32_t rot_dim, const void* dq_out,
+                                       const void* dk_out, void* dq, void* dk, void* dgamma_q,
+                                       void* dgamma_k, void* workspace, int64_t workspace_bytes,
+                                       void* stream);
+
 /* Human-readable name of a status code (static storage). */
 const char* dtp_status_string(dtp_status status);
 

@@ -20,6 +20,7 @@ HEADER = os.path.join(os.path.dirname(_HERE), "include", "dtp.h")
 
 DTP_BF16 = 0
 DTP_F32 = 1
+DTP_ACT_NONE, DTP_ACT_SILU, DTP_ACT_GELU = 0, 1, 2
 DTP_OK, DTP_ERR_INVALID_ARG, DTP_ERR_UNSUPPORTED, DTP_ERR_DEGENERATE, DTP_ERR_NO_MEMORY, DTP_ERR_HIP = (
     0, -1, -2, -3, -4, -5)
 
@@ -46,6 +47,7 @@ class dtp_ca_options(ctypes.Structure):
 _P = ctypes.c_void_p
 _I32 = ctypes.c_int32
 _I64 = ctypes.c_int64
+_F32 = ctypes.c_float
 _SIGNATURES = {
     "dtp_layer_create": (_I32, [ctypes.POINTER(dtp_layer_desc), ctypes.POINTER(_P)]),
     "dtp_layer_destroy": (_I32, [_P]),
@@ -74,6 +76,17 @@ _SIGNATURES = {
     "dtp_coordinate_ascent": (_I32, [_I32, _I32, _I32, _I32, _P, _P, ctypes.POINTER(dtp_ca_options),
                                      _P, _P, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(_I64),
                                      ctypes.POINTER(_I32), _P]),
+    "dtp_linear_workspace": (_I64, [_I64] + [_I32] * 5),
+    "dtp_linear_forward": (_I32, [_I64] + [_I32] * 3 + [_P] * 4 + [_I32, _F32] + [_P] * 3 + [_I64, _P]),
+    "dtp_linear_backward": (_I32, [_I64] + [_I32] * 3 + [_P] * 3 + [_I32, _F32] + [_P] * 5 + [_I64, _P]),
+    "dtp_gated_workspace": (_I64, [_I64] + [_I32] * 4),
+    "dtp_gated_forward": (_I32, [_I64] + [_I32] * 3 + [_P] * 3 + [_I32] + [_P] * 3 + [_I64, _P]),
+    "dtp_gated_backward": (_I32, [_I64] + [_I32] * 3 + [_P] * 3 + [_I32] + [_P] * 6 + [_I64, _P]),
+    "dtp_qk_norm_rotate_workspace": (_I64, [_I64] + [_I32] * 4),
+    "dtp_qk_norm_rotate_forward": (_I32, [_I64] + [_I32] * 4 + [_P, _I64, _P, _I64, _P, _P, _F32, _P, _P, _I32]
+                                   + [_P] * 3),
+    "dtp_qk_norm_rotate_backward": (_I32, [_I64] + [_I32] * 4 + [_P, _I64, _P, _I64, _P, _P, _F32, _P, _P, _I32]
+                                    + [_P] * 7 + [_I64, _P]),
     "dtp_status_string": (ctypes.c_char_p, [_I32]),
     "dtp_last_error": (ctypes.c_char_p, []),
 }
@@ -413,3 +426,127 @@ def dtp_apply_layout(d_model, n_neurons, n_q_heads, n_kv_groups, head_dim, dtype
     _check(lib().dtp_apply_layout(ctypes.byref(desc), L, _ptr(h), _ptr(nu),
                                   ctypes.cast(srcp, ctypes.c_void_p), ctypes.cast(dstp, ctypes.c_void_p),
                                   _stream(stream)))
+
+
+# ----------------------------------------------------------------------------- dense layer
+# Activations take the layer's dtype, `pre` float32.  `workspace`: a tensor on the GPU of at least
+# the bytes that the operator's _workspace function gives, or None (stream-ordered scratch).
+_F = ("float32",)
+
+
+def _work(workspace):
+    if workspace is None:
+        return None, 0
+    p = _dev(workspace, "workspace", ("uint8",), 0)
+    if isinstance(workspace, int):
+        raise TypeError("workspace must be a torch tensor on the GPU")
+    return p, workspace.numel()
+
+
+def dtp_linear_workspace(n_tokens, n_in, n_out, dtype, act=DTP_ACT_NONE, backward=False):
+    return int(lib().dtp_linear_workspace(n_tokens, n_in, n_out, int(dtype), int(act), int(bool(backward))))
+
+
+def dtp_linear_forward(n_tokens, n_in, n_out, dtype, x, w, y, bias=None, residual=None, act=DTP_ACT_NONE, alpha=1.0,
+                       pre=None, workspace=None, stream=None):
+    """y = residual + alpha act(x w^T + bias); `pre` (float32) keeps x w^T + bias."""
+    ad, T, K, N = _act_dtypes(dtype), n_tokens, n_in, n_out
+    _check(lib().dtp_linear_forward(T, K, N, int(dtype), _dev(x, "x", ad, T * K), _dev(w, "w", ad, N * K),
+                                    _dev(bias, "bias", ad, N, True), _dev(residual, "residual", ad, T * N, True),
+                                    int(act), alpha, _dev(y, "y", ad, T * N), _dev(pre, "pre", _F, T * N, True),
+                                    *_work(workspace), _stream(stream)))
+
+
+def dtp_linear_backward(n_tokens, n_in, n_out, dtype, x, w, dy, dx=None, dw=None, dbias=None, act=DTP_ACT_NONE,
+                        alpha=1.0, pre=None, workspace=None, stream=None):
+    """Gradients of dtp_linear_forward into those of dx, dw and dbias that are given."""
+    ad, T, K, N = _act_dtypes(dtype), n_tokens, n_in, n_out
+    _check(lib().dtp_linear_backward(T, K, N, int(dtype), _dev(x, "x", ad, T * K, dw is None),
+                                     _dev(w, "w", ad, N * K, dx is None), _dev(dy, "dy", ad, T * N), int(act), alpha,
+                                     _dev(pre, "pre", _F, T * N, act == DTP_ACT_NONE),
+                                     _dev(dx, "dx", ad, T * K, True), _dev(dw, "dw", ad, N * K, True),
+                                     _dev(dbias, "dbias", ad, N, True), *_work(workspace), _stream(stream)))
+
+
+def dtp_gated_workspace(n_tokens, d_model, n_neurons, dtype, backward=False):
+    return int(lib().dtp_gated_workspace(n_tokens, d_model, n_neurons, int(dtype), int(bool(backward))))
+
+
+def dtp_gated_forward(n_tokens, d_model, n_neurons, dtype, x, w_gate, w_up, h, act=DTP_ACT_SILU, pre=None,
+                      workspace=None, stream=None):
+    """h = act(x w_gate^T) (x w_up^T); `pre` (float32 [n_tokens, 2, n_neurons]) keeps both products."""
+    ad, T, d, I = _act_dtypes(dtype), n_tokens, d_model, n_neurons
+    _check(lib().dtp_gated_forward(T, d, I, int(dtype), _dev(x, "x", ad, T * d), _dev(w_gate, "w_gate", ad, I * d),
+                                   _dev(w_up, "w_up", ad, I * d), int(act), _dev(h, "h", ad, T * I),
+                                   _dev(pre, "pre", _F, 2 * T * I, True), *_work(workspace), _stream(stream)))
+
+
+def dtp_gated_backward(n_tokens, d_model, n_neurons, dtype, x, w_gate, w_up, pre, dh, dx=None, dw_gate=None,
+                       dw_up=None, act=DTP_ACT_SILU, workspace=None, stream=None):
+    """Gradients of dtp_gated_forward into dx, and into dw_gate and dw_up, as given."""
+    ad, T, d, I = _act_dtypes(dtype), n_tokens, d_model, n_neurons
+    no_dw = dw_gate is None and dw_up is None
+    _check(lib().dtp_gated_backward(T, d, I, int(dtype), _dev(x, "x", ad, T * d, no_dw),
+                                    _dev(w_gate, "w_gate", ad, I * d, dx is None),
+                                    _dev(w_up, "w_up", ad, I * d, dx is None), int(act),
+                                    _dev(pre, "pre", _F, 2 * T * I), _dev(dh, "dh", ad, T * I),
+                                    _dev(dx, "dx", ad, T * d, True), _dev(dw_gate, "dw_gate", ad, I * d, True),
+                                    _dev(dw_up, "dw_up", ad, I * d, True), *_work(workspace), _stream(stream)))
+
+
+def _heads(t, name, dtypes, n_tokens, heads, head_dim):
+    """(address, elements between tokens) of a [n_tokens, heads, head_dim] GPU tensor whose tokens may
+    lie apart, as a slice of a packed projection's rows does."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dim() != 3:
+        raise TypeError(f"{name} must be a torch tensor of 3 dimensions on the GPU")
+    if tuple(t.shape) != (n_tokens, heads, head_dim):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, the call needs {(n_tokens, heads, head_dim)}")
+    stride = t.stride(0) if n_tokens > 1 else heads * head_dim
+    if n_tokens:
+        if (t.stride(2) != 1 and head_dim > 1) or (t.stride(1) != head_dim and heads > 1):
+            raise ValueError(f"{name}: the heads of a token must be contiguous")
+        _dev(t[0], name, dtypes, 0)
+    return t.data_ptr(), stride
+
+
+def _rotation(positions, inv_freq, n_tokens):
+    if (positions is None) != (inv_freq is None):
+        raise ValueError("positions and inv_freq must be given together")
+    if positions is None:
+        return None, None, 0
+    import torch
+    if not isinstance(inv_freq, torch.Tensor):
+        raise TypeError("inv_freq must be a torch tensor on the GPU")
+    return (_dev(positions, "positions", ("int32",), n_tokens), _dev(inv_freq, "inv_freq", _F, 0),
+            2 * inv_freq.numel())
+
+
+def dtp_qk_norm_rotate_workspace(n_tokens, n_q_heads, n_kv_groups, head_dim, dtype):
+    return int(lib().dtp_qk_norm_rotate_workspace(n_tokens, n_q_heads, n_kv_groups, head_dim, int(dtype)))
+
+
+def dtp_qk_norm_rotate_forward(n_tokens, n_q_heads, n_kv_groups, head_dim, dtype, q, k, q_out, k_out, gamma_q=None,
+                               gamma_k=None, eps=1e-6, positions=None, inv_freq=None, stream=None):
+    """q [n_tokens, n_q_heads, head_dim] and k may be slices of a packed projection (their strides are
+    passed on); rotates the first 2 * len(inv_freq) columns of each head."""
+    ad, T, H, G, dh = _act_dtypes(dtype), n_tokens, n_q_heads, n_kv_groups, head_dim
+    _check(lib().dtp_qk_norm_rotate_forward(
+        T, H, G, dh, int(dtype), *_heads(q, "q", ad, T, H, dh), *_heads(k, "k", ad, T, G, dh),
+        _dev(gamma_q, "gamma_q", ad, dh, True), _dev(gamma_k, "gamma_k", ad, dh, True), eps,
+        *_rotation(positions, inv_freq, T), _dev(q_out, "q_out", ad, T * H * dh), _dev(k_out, "k_out", ad, T * G * dh),
+        _stream(stream)))
+
+
+def dtp_qk_norm_rotate_backward(n_tokens, n_q_heads, n_kv_groups, head_dim, dtype, q, k, dq_out, dk_out, dq, dk,
+                                gamma_q=None, gamma_k=None, eps=1e-6, positions=None, inv_freq=None, dgamma_q=None,
+                                dgamma_k=None, workspace=None, stream=None):
+    """Gradients of dtp_qk_norm_rotate_forward; q and k as it read them."""
+    ad, T, H, G, dh = _act_dtypes(dtype), n_tokens, n_q_heads, n_kv_groups, head_dim
+    _check(lib().dtp_qk_norm_rotate_backward(
+        T, H, G, dh, int(dtype), *_heads(q, "q", ad, T, H, dh), *_heads(k, "k", ad, T, G, dh),
+        _dev(gamma_q, "gamma_q", ad, dh, True), _dev(gamma_k, "gamma_k", ad, dh, True), eps,
+        *_rotation(positions, inv_freq, T), _dev(dq_out, "dq_out", ad, T * H * dh),
+        _dev(dk_out, "dk_out", ad, T * G * dh), _dev(dq, "dq", ad, T * H * dh), _dev(dk, "dk", ad, T * G * dh),
+        _dev(dgamma_q, "dgamma_q", ad, dh, True), _dev(dgamma_k, "dgamma_k", ad, dh, True), *_work(workspace),
+        _stream(stream)))
