@@ -339,7 +339,7 @@ dtp_status dtp_apply_layout(const dtp_layer_desc* desc, int32_t L, const int32_t
  *
  * Shared by these entry points:
  *   - Tensors are dense row-major in `dtype` unless said otherwise, every pointer 16-byte
- *     aligned.  Any sizes > 0 are taken, up to 2^20 features, 2^31 weights and 2^30 tokens
+ *     aligned.  Any sizes > 0 are taken, up to 2^20 features, 2^30 weights and 2^30 tokens
  *     (DTP_ERR_UNSUPPORTED beyond); multiples of 8 features need no padded copies.
  *     n_tokens == 0 is a no-op, except that gradients of weights are then zeros.
  *   - Sums are held in 32 bits or more and rounded to `dtype` once.  bf16 gradients of an

@@ -76,9 +76,11 @@ struct Workspace {
   dtp_status open(void* given, int64_t given_bytes, int64_t need, hipStream_t stream);
 };
 
-// Enqueues the product.  `partial`: workspace of product_partial_bytes(p) bytes.
-size_t product_partial_bytes(const Product& p);
-dtp_status launch_product(const Product& p, float* partial, hipStream_t s);
+// Enqueues the product; workspace of product_bytes(p) bytes, 256-byte pieces.
+size_t product_bytes(const Product& p);
+dtp_status launch_product(const Product& p, char* workspace, hipStream_t s);
+size_t product_bytes_bf16(const Product& p);  // dense_bf16.hip
+dtp_status launch_product_bf16(const Product& p, char* workspace, hipStream_t s);
 
 #ifdef __HIPCC__
 

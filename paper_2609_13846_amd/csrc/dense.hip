@@ -110,7 +110,7 @@ column_sums_kernel(const S* __restrict__ dy, const float* __restrict__ pre, int 
   __shared__ float sums[8][kSumCols];
   const int group = threadIdx.x % 32, lane = threadIdx.x / 32;
   const int n = blockIdx.x * kSumCols + 8 * group, count = N - n;
-  const int64_t t0 = blockIdx.y * rows, t1 = min(T, t0 + rows);
+  const int64_t t0 = blockIdx.y * rows, t1 = t0 + rows < T ? t0 + rows : T;
   float acc[8] = {};
   if (count > 0)
     for (int64_t t = t0 + lane; t < t1; t += 8) {
@@ -201,7 +201,7 @@ dtp_status launch_activation_grad(const void* dy, const float* pre, int act, flo
 // A call's products and the offsets of its buffers in the workspace.  The pointers of `Product`s
 // whose operand is a workspace buffer are set once the workspace is there.
 struct Plan {
-  size_t dz = 0, sums = 0, partial = 0, bytes = 0;
+  size_t dz = 0, sums = 0, scratch = 0, bytes = 0;
   int ld = 0;  // of dz
 };
 
@@ -255,6 +255,12 @@ Product dw_product(int64_t T, int K, int N, int parts, int ld, int dtype) {
   return p;
 }
 
+// Whether dz is formed on its own: with an activation, and where the bf16 kernels cannot take dy's
+// rows in 16-byte pieces.
+bool needs_pass(int N, int dtype, bool gated, bool with_act) {
+  return gated || with_act || (dtype == DTP_BF16 && N % 8 != 0);
+}
+
 Plan backward_plan(int64_t T, int K, int N, int parts, int dtype, bool pass, bool sums) {
   Plan w;
   w.ld = pass ? pad32(N) : N;
@@ -262,25 +268,26 @@ Plan backward_plan(int64_t T, int K, int N, int parts, int dtype, bool pass, boo
   if (pass) at = up256(esize(dtype) * (size_t)T * parts * w.ld);
   w.sums = at;
   if (sums) at += up256(sizeof(float) * (size_t)sum_chunks(T) * N);
-  w.partial = at;
-  w.bytes = at + std::max(product_partial_bytes(dx_product(T, K, N, parts, w.ld, dtype)),
-                          product_partial_bytes(dw_product(T, K, N, parts, w.ld, dtype)));
+  w.scratch = at;
+  w.bytes = at + std::max(product_bytes(dx_product(T, K, N, parts, w.ld, dtype)),
+                          product_bytes(dw_product(T, K, N, parts, w.ld, dtype)));
   return w;
 }
 
 dtp_status check_sizes(int64_t T, int32_t K, int32_t N, int dtype) {
   DTP_CHECK(T >= 0, DTP_ERR_INVALID_ARG, "n_tokens=%lld is negative", (long long)T);
   DTP_CHECK(K > 0 && N > 0, DTP_ERR_INVALID_ARG, "every size must be positive (%d features in, %d out)", K, N);
-  DTP_CHECK(T <= ((int64_t)1 << 30) && K <= (1 << 20) && N <= (1 << 20) && (int64_t)K * N <= ((int64_t)1 << 31),
-            DTP_ERR_UNSUPPORTED, "shape too large (tokens <= 2^30, features <= 2^20, weights <= 2^31)");
+  DTP_CHECK(T <= ((int64_t)1 << 30) && K <= (1 << 20) && N <= (1 << 20) && (int64_t)K * N <= ((int64_t)1 << 30),
+            DTP_ERR_UNSUPPORTED, "shape too large (tokens <= 2^30, features <= 2^20, weights <= 2^30)");
   DTP_CHECK(dtype == DTP_BF16 || dtype == DTP_F32, DTP_ERR_UNSUPPORTED, "dtype %d", dtype);
   return DTP_OK;
 }
 
 int64_t workspace_bytes(ProductKind kind, int64_t T, int K, int N, int dtype, int act, bool backward) {
   const int parts = kind == kProductGated ? 2 : 1;
-  size_t n = product_partial_bytes(forward_product(kind, T, K, N, dtype));
-  if (backward) n = std::max(n, backward_plan(T, K, N, parts, dtype, parts == 2 || act != DTP_ACT_NONE, parts == 1).bytes);
+  size_t n = product_bytes(forward_product(kind, T, K, N, dtype));
+  if (backward) n = std::max(n, backward_plan(T, K, N, parts, dtype, needs_pass(N, dtype, parts == 2, act != DTP_ACT_NONE),
+                                       parts == 1).bytes);
   return (int64_t)n;
 }
 
@@ -315,8 +322,8 @@ dtp_status forward(ProductKind kind, int64_t T, int K, int N, int dtype, const v
   p.out.alpha = alpha;
   p.out.act = act;
   Workspace ws;
-  if ((st = ws.open(workspace, given_bytes, (int64_t)product_partial_bytes(p), s)) != DTP_OK) return st;
-  return launch_product(p, (float*)ws.base, s);
+  if ((st = ws.open(workspace, given_bytes, (int64_t)product_bytes(p), s)) != DTP_OK) return st;
+  return launch_product(p, ws.base, s);
 }
 
 // Both backward passes; w.w1 and dw1 are the up projection's.
@@ -351,7 +358,7 @@ dtp_status backward(ProductKind kind, int64_t T, int K, int N, int dtype, const 
     if (dw1 && (st = fill_zeros(dw1, (int64_t)N * K, dtype, s)) != DTP_OK) return st;
     return db ? fill_zeros(db, N, dtype, s) : DTP_OK;
   }
-  const bool pass = gated || with_act;
+  const bool pass = needs_pass(N, dtype, gated, with_act);
   const Plan plan = backward_plan(T, K, N, parts, dtype, pass, !gated);
   Workspace ws;
   if ((st = ws.open(workspace, given_bytes, (int64_t)plan.bytes, s)) != DTP_OK) return st;
@@ -359,23 +366,24 @@ dtp_status backward(ProductKind kind, int64_t T, int K, int N, int dtype, const 
       (st = launch_column_sums(dy, pre, act, alpha, T, N, dtype, db, (float*)(ws.base + plan.sums), s)) != DTP_OK)
     return st;
   if (!dx && !dw0) return DTP_OK;
-  const void* dz = dy;  // without an activation alpha is left to the products
+  const void* dz = dy;
+  const float in_pass = with_act ? alpha : 1.0f;  // without an activation alpha is left to the products: dz is dy
   if (pass) {
     void* out_dz = ws.base + plan.dz;
     dz = out_dz;
     st = gated ? launch_activation_grad<true>(dy, pre, act, 1.0f, T, N, plan.ld, dtype, out_dz, s)
-               : launch_activation_grad<false>(dy, pre, act, alpha, T, N, plan.ld, dtype, out_dz, s);
+               : launch_activation_grad<false>(dy, with_act ? pre : nullptr, act, in_pass, T, N, plan.ld, dtype, out_dz, s);
     if (st != DTP_OK) return st;
   }
-  float* partial = (float*)(ws.base + plan.partial);
+  char* scratch = ws.base + plan.scratch;
   if (dx) {
     Product p = dx_product(T, K, N, parts, plan.ld, dtype);
     p.a0 = w.w0;
     p.a1 = w.w1;
     p.b = dz;
     p.out.y = dx;
-    p.out.alpha = pass ? 1.0f : alpha;
-    if ((st = launch_product(p, partial, s)) != DTP_OK) return st;
+    p.out.alpha = with_act ? 1.0f : alpha;
+    if ((st = launch_product(p, scratch, s)) != DTP_OK) return st;
   }
   if (dw0) {
     Product p = dw_product(T, K, N, parts, plan.ld, dtype);
@@ -383,8 +391,8 @@ dtp_status backward(ProductKind kind, int64_t T, int K, int N, int dtype, const 
     p.b = dz;
     p.out.y = dw0;
     p.out.y2 = dw1;
-    p.out.alpha = pass ? 1.0f : alpha;
-    if ((st = launch_product(p, partial, s)) != DTP_OK) return st;
+    p.out.alpha = with_act ? 1.0f : alpha;
+    if ((st = launch_product(p, scratch, s)) != DTP_OK) return st;
   }
   return DTP_OK;
 }

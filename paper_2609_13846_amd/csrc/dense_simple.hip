@@ -57,14 +57,12 @@ void launch(const Product& p, hipStream_t s) {
 
 }  // namespace
 
-size_t product_partial_bytes(const Product&) { return 0; }
+size_t product_bytes(const Product& p) { return p.dtype == DTP_BF16 ? product_bytes_bf16(p) : 0; }
 
-dtp_status launch_product(const Product& p, float*, hipStream_t s) {
+dtp_status launch_product(const Product& p, char* workspace, hipStream_t s) {
   if (p.N == 0) return DTP_OK;
-  if (p.dtype == DTP_BF16)
-    launch<uint16_t>(p, s);
-  else
-    launch<float>(p, s);
+  if (p.dtype == DTP_BF16) return launch_product_bf16(p, workspace, s);
+  launch<float>(p, s);
   DTP_HIP(hipGetLastError());
   return DTP_OK;
 }
