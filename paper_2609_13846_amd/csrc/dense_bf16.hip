@@ -17,13 +17,13 @@ constexpr int kCus = 256;
 
 struct TileArgs {
   const uint16_t *a0, *a1, *b;
-  int64_t lda, ldb;
+  RowContraction k;
+  int64_t K;          // columns of a segment
   int M, N, Mp;       // Mp: M rounded up to 8, the row of a partial sum
-  int64_t K;          // columns per segment
-  int nq_seg, nq;     // stages per segment, and of the whole contraction
-  int per;            // stages per split
+  int nq, per;        // stages (stream: runs of 64 columns) of the contraction, and of a split
   int m_tiles, n_tiles;
-  uint32_t b_jump;
+  int64_t bytes_a, bytes_b;  // of the operands
+  int64_t second_a;          // bytes from a0 to the second segment's matrix
   float* partial;     // [splits][planes][N][Mp], or NULL
   ProductOut out;
 };
@@ -34,52 +34,153 @@ __device__ __forceinline__ void store_partial(float* p, const float (&v)[W]) {
   for (int i = 0; i < W; i += 4) *reinterpret_cast<f32x4*>(p + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
 }
 
+__device__ __forceinline__ float half_of(const u32x4& v, int e) {
+  return __uint_as_float(e % 2 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16);
+}
+__device__ __forceinline__ void store_whole(uint16_t* p, const float (&v)[8]) {
+  u32x4 o;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
+  *reinterpret_cast<u32x4*>(p) = o;
+}
+
+// write_product for eight whole, aligned features.
+template <ProductKind KIND>
+__device__ __forceinline__ void write_whole(const ProductOut& o, int64_t n, int m, int M, const float (&c0)[8],
+                                            const float (&c1)[8], const u32x4& bias, const u32x4& residual) {
+  float v[8];
+  uint16_t *const y1 = (uint16_t*)o.y, *const y2 = (uint16_t*)o.y2;
+  if constexpr (KIND == kProductLinear) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = c0[e] + half_of(bias, e);
+    if (o.pre) store_partial(o.pre + n * M + m, v);
+    if (o.act != DTP_ACT_NONE) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = activate<uint16_t>(o.act, v[e]);
+    }
+    if (o.residual) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = fmaf(o.alpha, v[e], half_of(residual, e));
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] *= o.alpha;
+    }
+    store_whole((uint16_t*)o.y + n * M + m, v);
+  } else if constexpr (KIND == kProductGated) {
+    if (o.pre) {
+      store_partial(o.pre + 2 * n * M + m, c0);
+      store_partial(o.pre + (2 * n + 1) * M + m, c1);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = activate<uint16_t>(o.act, c0[e]) * c1[e];
+    store_whole((uint16_t*)o.y + n * M + m, v);
+  } else {
+    const bool second = n >= o.n_split;
+    const int64_t row = second ? n - o.n_split : n;
+    if (row >= o.n_keep) return;
+    uint16_t* const y = second ? y2 : y1;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = o.alpha * c0[e];
+    store_whole(y + row * M + m, v);
+  }
+}
+
+// One block per CU (256 x 256 tiles; two of 128 x 128), each with a run of items: a tile, or a split of
+// its contraction.  Items are numbered so that the ones that run together on an XCD share operands.
 template <int AF, int BF, bool AT, bool BT, ProductKind KIND>
 __global__ void __launch_bounds__(512, AF * BF > 16 ? 2 : 4) tile_product_kernel(TileArgs p) {
   constexpr bool kGated = KIND == kProductGated;
   using Pipe = RowPipe<AF, BF, AT, BT, kGated>;
-  constexpr int kTileM = kGated ? Pipe::kARows / 2 : Pipe::kARows, kTileN = Pipe::kBRows;
-  __shared__ __attribute__((aligned(16))) uint16_t s0[Pipe::kSlot], s1[Pipe::kSlot], s2[Pipe::kSlot], s3[Pipe::kSlot];
-  int tm, tn;
-  frag_work(blockIdx.x, p.m_tiles, p.n_tiles, 8, tm, tn);
-  const int m0 = tm * kTileM, n0 = tn * kTileN;
-  const int q0 = blockIdx.y * p.per, q1 = min(q0 + p.per, p.nq);
-  const bool rebase = p.nq == p.nq_seg;  // one segment: pointers at the split's first stage
-  const int64_t first = rebase ? (int64_t)q0 * 32 : 0;
-  auto operand = [&](const uint16_t* x, const uint16_t* x2, int64_t ld, bool across, int row, int64_t rows) {
-    const int64_t o = across ? first * ld + row : (int64_t)row * ld + first;
-    const int64_t left = 2 * ((across ? p.K : rows) * ld - o);
-    return RowOperand{x + o, x2 ? x2 + o : nullptr, ld, left < (int64_t)kRowRange ? (uint32_t)left : kRowRange};
-  };
-  Pipe pipe(operand(p.a0, p.a1, p.lda, AT, m0, p.M), operand(p.b, nullptr, p.ldb, BT, n0, p.N), p.b_jump);
-  pipe.contract(s0, s1, s2, s3, q0, q1, p.nq_seg, p.K, rebase ? q0 : 0);
-
+  constexpr int kTileM = kGated ? Pipe::kHalf : Pipe::kARows, kTileN = Pipe::kBRows;
   constexpr int kPairs = kGated ? AF / 4 : AF / 2;
-  const int planes = kGated ? 2 : 1;
-  const int m_lane = m0 + pipe.wm * (kGated ? 8 * AF : 16 * AF) + 8 * (pipe.lane / 16);
-#pragma unroll
-  for (int j = 0; j < BF; ++j) {
-    const int n = n0 + pipe.wn * 16 * BF + 16 * j + pipe.lane % 16;
-    if (n >= p.N) continue;
-#pragma unroll
-    for (int i = 0; i < kPairs; ++i) {
-      const int m = m_lane + 32 * i;
-      float c0[8], c1[8];
+  __shared__ __attribute__((aligned(16))) uint16_t s0a0[Pipe::kASlot], s0a1[Pipe::kASlot], s0b[Pipe::kBSlot],
+      s1a0[Pipe::kASlot], s1a1[Pipe::kASlot], s1b[Pipe::kBSlot];
+  const int tiles = p.m_tiles * p.n_tiles;
+  auto place = [&](int i, int& m0, int& n0, int& split) __attribute__((always_inline)) {
+    split = i / tiles;
+    int tm, tn;
+    frag_work(i - split * tiles, p.m_tiles, p.n_tiles, 8, tm, tn);
+    m0 = tm * kTileM;
+    n0 = tn * kTileN;
+  };
+  auto item = [&](int i) __attribute__((always_inline)) {
+    int m0, n0, split;
+    place(i, m0, n0, split);
+    RowItem it;
+    it.first = split * p.per;
+    it.n = min(p.per, p.nq - it.first);
+    const bool second = it.first >= p.k.per_segment;
+    const int64_t in_seg = second ? it.first - p.k.per_segment : it.first;
+    const int64_t oa = (AT ? m0 : m0 * (int64_t)p.k.lda) * 2 + in_seg * p.k.step_a;
+    const int64_t ob = (BT ? n0 : n0 * (int64_t)p.k.ldb) * 2 + it.first * p.k.step_b + (second ? p.k.jump_b : 0);
+    it.a = (const char*)p.a0 + (second ? p.second_a : 0) + oa;
+    it.left_a = p.bytes_a - oa;
+    it.b = (const char*)p.b + ob;
+    it.left_b = p.bytes_b - ob;
+    it.columns = p.k.columns - (int)in_seg * kRowStage;
+    return it;
+  };
+  Pipe pipe(p.k);
+  auto done = [&](int i) __attribute__((always_inline)) {
+    int m0, n0, split;
+    place(i, m0, n0, split);
+    const int m_lane = m0 + pipe.wm * (kGated ? 8 * AF : 16 * AF) + 8 * (pipe.lane / 16);
+    const int n_lane = n0 + pipe.wn * 16 * BF + pipe.lane % 16;
+    auto sums = [&](int i, int j, float (&c0)[8], float (&c1)[8]) __attribute__((always_inline)) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         c0[e] = pipe.acc[2 * i + e / 4][j][e % 4];
         c1[e] = kGated ? pipe.acc[kGated ? AF / 2 + 2 * i + e / 4 : 0][j][e % 4] : 0.0f;
       }
-      if (p.partial) {
-        if (m >= p.M) continue;
-        float* at = p.partial + ((int64_t)blockIdx.y * planes * p.N + n) * p.Mp + m;
-        store_partial(at, c0);
-        if (kGated) store_partial(at + (int64_t)p.N * p.Mp, c1);
-      } else {
-        write_product<uint16_t, KIND, 8>(p.out, n, m, p.M, c0, c1);
+    };
+    if (p.partial) {
+      const int planes = kGated ? 2 : 1;
+#pragma unroll
+      for (int j = 0; j < BF; ++j)
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) {
+          const int n = n_lane + 16 * j, m = m_lane + 32 * i;
+          if (n >= p.N || m >= p.M) continue;
+          float c0[8], c1[8];
+          sums(i, j, c0, c1);
+          float* at = p.partial + ((int64_t)split * planes * p.N + n) * p.Mp + m;
+          store_partial(at, c0);
+          if (kGated) store_partial(at + (int64_t)p.N * p.Mp, c1);
+        }
+      return;
+    }
+    // results a row at a time, the next row's residual on its way beside this one's writes
+    constexpr bool kLinear = KIND == kProductLinear;
+    u32x4 bias[kPairs] = {}, residual[2][kPairs] = {};
+    if (kLinear && p.out.bias) {
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i)
+        if (m_lane + 32 * i < p.M) bias[i] = *reinterpret_cast<const u32x4*>((const uint16_t*)p.out.bias + m_lane + 32 * i);
+    }
+    auto fetch = [&](int j) __attribute__((always_inline)) {
+      if (!kLinear || !p.out.residual || n_lane + 16 * j >= p.N) return;
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i)
+        if (m_lane + 32 * i < p.M)
+          residual[j % 2][i] = *reinterpret_cast<const u32x4*>((const uint16_t*)p.out.residual +
+                                                               (int64_t)(n_lane + 16 * j) * p.M + m_lane + 32 * i);
+    };
+    fetch(0);
+#pragma unroll
+    for (int j = 0; j < BF; ++j) {
+      if (j + 1 < BF) fetch(j + 1);
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i) {
+        const int n = n_lane + 16 * j, m = m_lane + 32 * i;
+        if (n >= p.N || m >= p.M) continue;
+        float c0[8], c1[8];
+        sums(i, j, c0, c1);
+        write_whole<KIND>(p.out, n, m, p.M, c0, c1, bias[i], residual[j % 2][i]);
       }
     }
-  }
+  };
+  const int items = tiles * ((p.nq + p.per - 1) / p.per);
+  pipe.run({s0a0, s0a1, s0b}, {s1a0, s1a1, s1b}, blockIdx.x, items, gridDim.x, item, done);
 }
 
 // Few tokens (at most 16 TF): the time is that of reading the weights once.  A block takes 16
@@ -96,11 +197,11 @@ __global__ void __launch_bounds__(512) stream_product_kernel(TileArgs p) {
   const int r = lane % 16, g = lane / 16;
   const int m0 = blockIdx.x * 16, m = min(m0 + r, p.M - 1);
   const uint16_t* a[kMats];
-  a[0] = p.a0 + (int64_t)m * p.lda + 16 * g;
-  if constexpr (kGated) a[1] = p.a1 + (int64_t)m * p.lda + 16 * g;
+  a[0] = p.a0 + (int64_t)m * p.k.lda + 16 * g;
+  if constexpr (kGated) a[1] = p.a1 + (int64_t)m * p.k.lda + 16 * g;
   const uint16_t* b[TF];
 #pragma unroll
-  for (int t = 0; t < TF; ++t) b[t] = p.b + (int64_t)min(16 * t + r, p.N - 1) * p.ldb + 16 * g;
+  for (int t = 0; t < TF; ++t) b[t] = p.b + (int64_t)min(16 * t + r, p.N - 1) * p.k.ldb + 16 * g;
   f32x4 acc[kMats][TF] = {};
   const int c0 = blockIdx.y * p.per, c1 = min(c0 + p.per, p.nq);  // runs
   const int whole = min(c1, (int)(p.K / 64));
@@ -218,7 +319,7 @@ __global__ void __launch_bounds__(256) pad_rows_kernel(const uint16_t* __restric
 struct Shape {
   bool stream = false;
   int tile = 256;      // rows and columns of a tile
-  int splits = 1, per = 0, nq = 0, nq_seg = 0;
+  int splits = 1, per = 0, nq = 0;
 };
 
 Shape choose(const Product& p) {
@@ -226,24 +327,19 @@ Shape choose(const Product& p) {
   const bool gated = p.kind == kProductGated;
   if (!p.at && !p.bt && p.N <= 64) {
     s.stream = true;
-    s.nq = s.nq_seg = (int)((p.K + 63) / 64);
+    s.nq = (int)((p.K + 63) / 64);
     const int rows = (p.M + 15) / 16;
     int splits = 1;
     while (rows * splits < kCus / 2 && s.nq / (splits * 2) >= 16) splits *= 2;
     s.per = (s.nq + splits - 1) / splits;
   } else {
-    s.nq_seg = (int)((p.K + 31) / 32);
-    s.nq = s.nq_seg * p.segments;
+    s.nq = (int)((p.K + 2 * kRowStage - 1) / (2 * kRowStage)) * 2 * p.segments;
     auto tiles = [&](int t) { return ((int64_t)(gated ? 2 : 1) * p.M + t - 1) / t * ((p.N + t - 1) / t); };
     s.tile = tiles(256) >= 192 ? 256 : 128;
+    if (p.bt && tiles(256) * (s.nq / 8) >= 192) s.tile = 256;
     const int64_t n = tiles(s.tile), room = s.tile == 256 ? kCus : 2 * kCus;
-    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({room / n, s.nq / 8, 16}));
-    s.per = (int)((s.nq + splits - 1) / splits);
-    // what a block reaches of an operand across has 31 bits
-    if (p.at || p.bt) {
-      const int64_t line = 64 * std::max(p.at ? p.lda : 0, p.bt ? p.ldb : 0);
-      if (p.segments == 1) s.per = (int)std::min<int64_t>(s.per, (int64_t)(kRowRange - 1) / line);
-    }
+    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({n >= room / 2 && !p.bt ? 1 : (3 * room + n - 1) / n, s.nq / 4, 16}));
+    s.per = (int)((s.nq / 2 + splits - 1) / splits) * 2;
   }
   s.splits = (s.nq + s.per - 1) / s.per;
   return s;
@@ -261,8 +357,12 @@ struct Lines {
 Lines lines_a(const Product& p) { return {p.at ? p.K : p.M, p.at ? p.M : p.K, p.lda % 8 != 0}; }
 Lines lines_b(const Product& p) { return {p.bt ? p.K : p.N, p.bt ? p.N : p.K, p.ldb % 8 != 0}; }
 
+// Split contractions meet in the join, and results whose rows are not whole 16-byte pieces are written
+// by it.
+bool uses_partial(const Product& p, const Shape& s) { return s.splits > 1 || (!s.stream && !p.out.vec); }
+
 size_t partial_bytes(const Product& p, const Shape& s) {
-  if (s.splits == 1) return 0;
+  if (!uses_partial(p, s)) return 0;
   return sizeof(float) * (size_t)s.splits * (p.kind == kProductGated ? 2 : 1) * (size_t)p.N * ((p.M + 7) / 8 * 8);
 }
 
@@ -278,8 +378,13 @@ const uint16_t* padded(const void* in, const Lines& l, char*& at, hipStream_t s)
 }
 
 template <ProductKind KIND, bool AT, bool BT>
-void launch_tiles(const TileArgs& t, const Shape& s, hipStream_t stream) {
-  const dim3 grid(t.m_tiles * t.n_tiles, s.splits);
+void launch_tiles(TileArgs& t, const Shape& s, hipStream_t stream) {
+  if (KIND == kProductGated) {
+    t.k.half_a = (const char*)t.a1 - (const char*)t.a0;
+  } else {
+    t.k.half_a = t.k.half_left = (s.tile == 256 ? 128 : 64) * (AT ? 1 : (int64_t)t.k.lda);  // 8 AF rows
+  }
+  const int items = t.m_tiles * t.n_tiles * s.splits, grid = std::min(items, s.tile == 256 ? kCus : 2 * kCus);
   if (s.tile == 256)
     tile_product_kernel<8, 4, AT, BT, KIND><<<grid, 512, 0, stream>>>(t);
   else
@@ -320,17 +425,26 @@ dtp_status launch_product_bf16(const Product& p, char* workspace, hipStream_t s)
   t.a1 = padded(p.a1, la, workspace, s);
   t.b = padded(p.b, lb, workspace, s);
   DTP_HIP(hipGetLastError());
-  t.lda = la.pad ? pad32(la.n) : p.lda;
-  t.ldb = lb.pad ? pad32(lb.n) : p.ldb;
+  t.K = p.K;
+  t.k.lda = (uint32_t)(la.pad ? pad32(la.n) : p.lda);
+  t.k.ldb = (uint32_t)(lb.pad ? pad32(lb.n) : p.ldb);
+  t.bytes_a = 2 * la.rows * (int64_t)t.k.lda;
+  t.bytes_b = 2 * lb.rows * (int64_t)t.k.ldb;
+  t.k.step_a = 2 * kRowStage * (p.at ? (int64_t)t.k.lda : 1);
+  t.k.step_b = 2 * kRowStage * (p.bt ? (int64_t)t.k.ldb : 1);
+  t.k.per_segment = shape.nq / p.segments;
+  t.k.columns = (int)p.K;
+  if (p.segments == 2) {
+    t.second_a = (const char*)t.a1 - (const char*)t.a0;
+    t.k.jump_a = t.second_a - t.k.per_segment * t.k.step_a;
+    t.k.jump_b = 2 * p.b_seg - t.k.per_segment * t.k.step_b;
+  }
   t.M = p.M;
   t.N = (int)p.N;
   t.Mp = (p.M + 7) / 8 * 8;
-  t.K = p.K;
-  t.nq_seg = shape.nq_seg;
   t.nq = shape.nq;
   t.per = shape.per;
-  t.b_jump = (uint32_t)(2 * p.b_seg);
-  t.partial = shape.splits > 1 ? (float*)workspace : nullptr;
+  t.partial = uses_partial(p, shape) ? (float*)workspace : nullptr;
   t.out = p.out;
   if (shape.stream) {
     p.kind == kProductGated ? launch_stream<kProductGated>(t, shape, s) : launch_stream<kProductLinear>(t, shape, s);

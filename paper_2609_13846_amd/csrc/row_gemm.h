@@ -4,19 +4,33 @@
 // An operand is "along": element (row, k) at [row * ld + k], or "across": at [k * ld + row].
 // Whatever its order, a copy instruction moves 64 pieces of 16 bytes, and the lanes choose which
 // piece of the source each takes, so that the swizzle of the LDS image costs nothing:
-//   along   an LDS row of 32 columns (64 bytes) per operand row, its four pieces exchanged by the
+//   along   an LDS row of 64 columns (128 bytes) per operand row, its eight pieces exchanged by the
 //           row's number, so that the 16 rows of a fragment lie in different banks;
-//   across  an LDS line of all the tile's rows per contraction index, its pairs of pieces
-//           exchanged by the line's number, and the fragments read with the transposing LDS read:
-//           16 lanes take 4 lines x 16 rows and each gets the 4 lines of its row.
+//   across  an LDS line of all the rows per contraction index, its pairs of pieces exchanged by the
+//           line's number, and the fragments read with the transposing LDS read: 16 lanes take
+//           4 lines x 16 rows and each gets the 4 lines of its row.
+// Both read whole 128-byte lines of memory.  (Stages of 32 columns, 64 bytes of a row at a time, had
+// every line fetched twice from L2: 1,284 TFLOP/s for 8,192 x 4,096 x 28,672, both along.)
 // Reads past the operand return zeros (the buffer's range for rows and lines behind the last, an
 // address out of range for the columns behind a row's last): sizes need not be whole tiles.
 //
 // Rows of A are dealt to fragments so that a lane holds eight consecutive ones of a result's row:
-// fragments 2p and 2p + 1 take rows 8 r / 4 + r % 4 and + 4 of 32 (r: the row in the fragment).
+// fragments 2p and 2p + 1 take rows 8 (r / 4) + r % 4 and + 4 of 32 (r: the row in the fragment).
 //
-// The loop is that of FragPipe (frag_gemm.h): eight wavefronts, 2 along A x 4 along B, four slots
-// of 32 columns, one barrier per stage between the two halves of its products.
+// The loop: eight wavefronts, 2 along A x 4 along B, each AF x BF tiles of 16 x 16; stages of 64
+// columns in two LDS slots.  A wavefront's A fragments come in two halves, and a stage is four
+// steps of AF / 2 x BF products:
+//   1  half 0, columns  0-31   reads half 0, columns 32-63, and B's columns 32-63
+//                              copies half 1 of the next stage
+//   X  barrier: all have read half 0 and B; half 1 has landed
+//   2  half 0, columns 32-63   reads half 1, columns  0-31;  copies half 0, two stages on
+//   3  half 1, columns  0-31   reads half 1, columns 32-63;  copies B, two stages on
+//   Y  barrier: all have read half 1; the next stage's half 0 and B have landed
+//   4  half 1, columns 32-63   reads the next stage's first fragments;  copies the rest of B
+// so that every fragment is read a step before its products, a copy has three to five steps to
+// land, and the copies, which a wavefront cannot pass while the path to L2 is busy, are shared out
+// evenly.  The stages of a block's items follow each other without a gap: the copies run ahead
+// into the next item while the results of this one are written.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -28,12 +42,12 @@
 namespace dtp {
 
 typedef __attribute__((ext_vector_type(4))) short s16x4;
-typedef __attribute__((ext_vector_type(8))) short s16x8;
 
-constexpr uint32_t kRowRange = 0x80000000u;    // most bytes of an operand that a block may reach
+constexpr int kRowStage = 64;                  // columns per stage
+constexpr uint32_t kRowRange = 0x80000000u;    // most bytes of an operand that a stage may reach
 constexpr uint32_t kOutOfRange = 0xc0000000u;  // an offset beyond any range
 
-// Exchange of an across-line's pairs of pieces, so that lines 8 g + 0 .. 3 of all g, which one
+// Exchange of an across-line's pairs of pieces, so that the lines 8 g + 0 .. 3 of all g, which one
 // transposing read of a wavefront takes, lie in different banks.
 template <int ROWS>
 __device__ __forceinline__ int across_swizzle(int line) {
@@ -41,145 +55,161 @@ __device__ __forceinline__ int across_swizzle(int line) {
   if constexpr (ROWS == 128) return (line & 3) | ((line >> 3) & 1) << 2;
   return ((line >> 1) & 1) | ((line >> 3) & 1) << 1;
 }
+// Exchange of an along-row's pieces: the 16 rows of an A fragment (8 (r / 4) + r % 4), and of a B
+// fragment (r), take each of the eight pieces' places twice, once per 128 bytes of the banks.
+__device__ __forceinline__ int along_swizzle_a(int row) {
+  return (((row >> 1) & 1) | ((row >> 3) & 3) << 1) ^ ((row & 1) << 2);
+}
+__device__ __forceinline__ int along_swizzle_b(int row) { return ((row >> 1) & 7) ^ ((row & 1) << 2); }
 
-struct RowOperand {
-  const uint16_t* p;   // the block's first row and column
-  const uint16_t* p2;  // of the second segment (or of the second half of A's rows)
-  int64_t ld;
-  uint32_t range;      // bytes from p on that the block may read
+// Where an item's stages are.  `left`: bytes of the operand from the pointer on.
+struct RowItem {
+  const char *a, *b;  // the item's first row and first stage
+  int64_t left_a, left_b;
+  int columns;        // left of the segment
+  int first, n;       // its first stage's number in the whole contraction, and how many: an even number
 };
 
-// HALVES: A's rows come from two matrices, the first half of the tile's from p, the others from p2.
+// The contraction, all in bytes but for the counts: stages of one segment, or of a first and a second
+// one that starts jump_a and jump_b behind the end of the first.
+struct RowContraction {
+  uint32_t lda, ldb;       // elements
+  int64_t step_a, step_b;  // from stage to stage
+  int64_t half_a;          // from the first half of A's rows to the second (of another matrix: gated)
+  int64_t half_left;       // bytes less from there on
+  int64_t jump_a, jump_b;
+  int columns;             // of a segment
+  int per_segment;         // stages, an even number: the last one may have no columns
+};
+
+// HALVES: the halves of A's rows are 16 AF consecutive rows each (of two matrices).  Otherwise each
+// wavefront's rows are consecutive: half h of its 16 AF rows is 8 AF of them.
 template <int AF, int BF, bool AT, bool BT, bool HALVES>
 struct RowPipe {
-  static constexpr int kAFrags = 2 * AF, kBFrags = 4 * BF, kFrags = kAFrags + kBFrags;
-  static constexpr int kARows = 16 * kAFrags, kBRows = 16 * kBFrags;
-  static constexpr int kSlot = kFrags * 512;  // bf16 per LDS slot
-  static constexpr int kCopies = kFrags > 16 ? 4 : 2;  // copies per copying wavefront and stage
-  static constexpr int kH0 = AF / 2, kH1 = AF - kH0;
+  static constexpr int kARows = 32 * AF, kHalf = kARows / 2, kBRows = 64 * BF;
+  static constexpr int kASlot = kHalf * kRowStage, kBSlot = kBRows * kRowStage;  // bf16 per slot
+  static constexpr int kACopies = kHalf / 64, kBCopies = kBRows / 64;  // per wavefront: a half's, and B's
+  static constexpr int kCopies = 2 * kACopies + kBCopies;
+  static constexpr int kH = AF / 2;
   static constexpr int kReadsA = AT ? 2 : 1, kReadsB = BT ? 2 : 1;  // LDS reads per fragment
-  static_assert(kAFrags % kCopies == 0 && kBFrags % kCopies == 0 && kFrags <= 8 * kCopies, "copies share out");
-  static_assert(!HALVES || (!AT && (kAFrags / 2) % kCopies == 0 && AF % 4 == 0), "halves share out");
+  static_assert(kCopies < 16, "vmcnt field");
+
+  struct Slot {
+    uint16_t *a0, *a1, *b;
+  };
 
   int wave, lane, wm, wn;
-  bool copies_a;
-  const uint16_t *src, *src2;
-  uint32_t range;
-  uint32_t step, jump;      // bytes per stage; of the second segment's first stage
-  uint32_t voff[kCopies];
-  int piece[2];             // first column of an even and an odd copy's pieces (along)
-  int slot_copy;            // first copy's place in a slot, in 512s
-  int a_at, b_at;           // a fragment's place in a slot (along)
-  int a_line[AT ? AF / 2 : 1], b_line[BT ? BF : 1];  // (across)
+  const RowContraction& k;
+  uint32_t va[kACopies], vb[kBCopies];  // byte offsets of this lane's pieces
+  int piece_a, piece_b;                 // (along) first column of the first copy's piece
+  int a_at, b_at;                       // a fragment's place in a slot (along)
+  int a_line[AT ? kH / 2 : 1], b_line[BT ? BF : 1];  // (across)
   f32x4 acc[AF][BF];
-  bf16x8 a0[kH0], a1[kH1], b[BF];
+  bf16x8 ax[kH], ay[kH], b0[BF], b1[BF];
 
-  __device__ __forceinline__ RowPipe(const RowOperand& a, const RowOperand& bm, uint32_t b_jump) {
+  __device__ __forceinline__ static int source_row(int row) {
+    return HALVES ? row : row / (8 * AF) * (16 * AF) + row % (8 * AF);
+  }
+
+  __device__ __forceinline__ explicit RowPipe(const RowContraction& c) : k(c) {
     wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     lane = threadIdx.x & 63;
     wm = wave & 1;
     wn = wave >> 1;
-    const int w = min(wave, kFrags / kCopies - 1);
-    copies_a = w < kAFrags / kCopies;
-    const int c0 = kCopies * w - (copies_a ? 0 : kAFrags);  // its first copy in the operand
-    slot_copy = kCopies * w;
-    const int64_t ld = copies_a ? a.ld : bm.ld;
-    src = copies_a ? a.p : bm.p;
-    src2 = copies_a ? a.p2 : bm.p;
-    range = copies_a ? a.range : bm.range;
-    int row0 = 0;
-    if (HALVES && copies_a && c0 >= kAFrags / 2) {
-      src = a.p2;
-      row0 = kARows / 2;
-    }
-    const bool across = copies_a ? AT : BT;
-    step = across ? (uint32_t)ld * 64u : 64u;
-    jump = copies_a ? 0u : b_jump;
-    piece[0] = piece[1] = 0;
+    const uint32_t lda = k.lda, ldb = k.ldb;
+    piece_a = piece_b = 0;
 #pragma unroll
-    for (int j = 0; j < kCopies; ++j) {
-      const int c = c0 + j;
-      if (copies_a) {
-        if constexpr (AT) {
-          voff[j] = across_offset<kARows>(c, ld);
-        } else {
-          const int row = 16 * c + lane / 4;
-          const int s = (2 * ((row >> 1) & 1)) ^ ((row >> 3) & 3);
-          voff[j] = (uint32_t)(row - row0) * (uint32_t)ld * 2u + (uint32_t)((lane % 4) ^ s) * 16u;
-          if (j < 2) piece[j] = 8 * ((lane % 4) ^ s);
-        }
+    for (int j = 0; j < kACopies; ++j) {
+      const int c0 = wave * kACopies + j;
+      if constexpr (AT) {
+        const int at = c0 * 512 + lane * 8, line = at / kHalf;
+        const int row = 8 * ((at % kHalf / 8) ^ (2 * across_swizzle<kHalf>(line)));
+        va[j] = (uint32_t)line * lda * 2u + (uint32_t)source_row(row) * 2u;
       } else {
-        if constexpr (BT) {
-          voff[j] = across_offset<kBRows>(c, ld);
-        } else {
-          const int row = 16 * c + lane / 4;
-          const int s = (row >> 1) & 3;
-          voff[j] = (uint32_t)row * (uint32_t)ld * 2u + (uint32_t)((lane % 4) ^ s) * 16u;
-          if (j < 2) piece[j] = 8 * ((lane % 4) ^ s);
-        }
+        const int row = 8 * c0 + lane / 8, p = (lane % 8) ^ along_swizzle_a(row);
+        va[j] = (uint32_t)source_row(row) * lda * 2u + (uint32_t)p * 16u;
+        if (j == 0) piece_a = 8 * p;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kBCopies; ++j) {
+      const int c0 = wave * kBCopies + j;
+      if constexpr (BT) {
+        const int at = c0 * 512 + lane * 8, line = at / kBRows;
+        const int row = 8 * ((at % kBRows / 8) ^ (2 * across_swizzle<kBRows>(line)));
+        vb[j] = (uint32_t)line * ldb * 2u + (uint32_t)row * 2u;
+      } else {
+        const int row = 8 * c0 + lane / 8, p = (lane % 8) ^ along_swizzle_b(row);
+        vb[j] = (uint32_t)row * ldb * 2u + (uint32_t)p * 16u;
+        if (j == 0) piece_b = 8 * p;
       }
     }
     const int r = lane % 16, g = lane / 16;
-    const int rows_a = wm * (HALVES ? 8 * AF : 16 * AF);
+    a_at = b_at = a_line[0] = b_line[0] = 0;
     if constexpr (AT) {
-      const int s = across_swizzle<kARows>(8 * g + r / 4);
+      const int s = 2 * across_swizzle<kHalf>(8 * g + r / 4);
 #pragma unroll
-      for (int p = 0; p < AF / 2; ++p)
-        a_line[p] = (8 * g + r / 4) * kARows + (((rows_a + 32 * p) / 8 + r % 4) ^ (2 * s)) * 8;
-      a_at = 0;
+      for (int p = 0; p < kH / 2; ++p)
+        a_line[p] = (8 * g + r / 4) * kHalf + (((wm * 8 * AF + 32 * p) / 8 + r % 4) ^ s) * 8;
     } else {
-      a_at = (rows_a + 8 * (r / 4) + r % 4) * 32 + ((g ^ (2 * ((r >> 1) & 1)) ^ (r >> 2)) * 8);
-      a_line[0] = 0;
+      const int row = wm * 8 * AF + 8 * (r / 4) + r % 4;
+      a_at = row * kRowStage + (g ^ along_swizzle_a(row)) * 8;
     }
     if constexpr (BT) {
-      const int s = across_swizzle<kBRows>(8 * g + r / 4);
+      const int s = 2 * across_swizzle<kBRows>(8 * g + r / 4);
 #pragma unroll
       for (int j = 0; j < BF; ++j)
-        b_line[j] = kARows * 32 + (8 * g + r / 4) * kBRows + (((wn * 16 * BF + 16 * j) / 8 + r % 4 / 2) ^ (2 * s)) * 8 +
-                    4 * (r % 2);
-      b_at = 0;
+        b_line[j] = (8 * g + r / 4) * kBRows + (((wn * 16 * BF + 16 * j) / 8 + r % 4 / 2) ^ s) * 8 + 4 * (r % 2);
     } else {
-      b_at = kARows * 32 + (wn * 16 * BF + r) * 32 + ((g ^ ((r >> 1) & 3)) * 8);
-      b_line[0] = 0;
+      const int row = wn * 16 * BF + r;
+      b_at = row * kRowStage + (g ^ along_swizzle_b(row)) * 8;
     }
   }
 
-  // Byte offset of this lane's piece of copy c of an across operand.
-  template <int ROWS>
-  __device__ __forceinline__ uint32_t across_offset(int c, int64_t ld) const {
-    const int at = c * 512 + lane * 8, line = at / ROWS, p = at % ROWS / 8;
-    return (uint32_t)line * (uint32_t)ld * 2u + (uint32_t)(p ^ (2 * across_swizzle<ROWS>(line))) * 16u;
-  }
-
-  struct Stage {
-    int q;       // stage in its segment
-    bool second;
-    int columns;  // left of the segment from the stage's first on
+  // The stage that the copies are at.
+  struct Feed {
+    RowItem at;  // moved on from stage to stage; n: stages left
+    int index;
   };
 
-  __device__ __forceinline__ void copy(uint16_t* slot, Stage at) const {
-    int w = slot_copy;
-    asm("" : "+s"(w) : "s"(at.q));
-    w = __builtin_amdgcn_readfirstlane(w);
-    const uint16_t* base = (!HALVES && at.second) ? src2 : src;
-    const __amdgpu_buffer_rsrc_t rsrc = frag_rsrc(base, range);
-    const uint32_t off = (uint32_t)at.q * step + (at.second ? jump : 0u);
-    const bool along = copies_a ? !AT : !BT;
-    // columns behind the row's last are none of this row's
-    const bool out0 = along && piece[0] >= at.columns, out1 = along && piece[1] >= at.columns;
+  // A descriptor of `left` bytes; of none where nothing is left.
+  __device__ __forceinline__ static __amdgpu_buffer_rsrc_t stage_rsrc(const char* p, int64_t left) {
+    return frag_rsrc(p, left < 0 ? 0u : (left < (int64_t)kRowRange ? (uint32_t)left : kRowRange));
+  }
+  __device__ __forceinline__ void copy_a(uint16_t* slot, const Feed& f, int half) const {
+    const __amdgpu_buffer_rsrc_t rsrc =
+        stage_rsrc(f.at.a + (half ? k.half_a : 0), f.at.left_a - (half ? k.half_left : 0));
 #pragma unroll
-    for (int j = 0; j < kCopies; ++j)
+    for (int j = 0; j < kACopies; ++j) {
+      const bool out = !AT && (piece_a ^ (16 * j)) >= f.at.columns;  // columns behind the row's last
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          rsrc, (__attribute__((address_space(3))) void*)(slot + (w + j) * 512), 16,
-          (int)((AT && BT) ? voff[j] : ((j % 2 ? out1 : out0) ? kOutOfRange : voff[j])),
-          __builtin_amdgcn_readfirstlane((int)off), 0, 0);
+          rsrc, (__attribute__((address_space(3))) void*)(slot + (kACopies * wave + j) * 512), 16,
+          (int)(out ? kOutOfRange : va[j]), 0, 0, 0);
+    }
+  }
+  // Half `half` of the wavefront's copies of B.
+  __device__ __forceinline__ void copy_b(uint16_t* slot, const Feed& f, int half) const {
+    const __amdgpu_buffer_rsrc_t rsrc = stage_rsrc(f.at.b, f.at.left_b);
+#pragma unroll
+    for (int j = half * (kBCopies / 2); j < (half + 1) * (kBCopies / 2); ++j) {
+      const bool out = !BT && (piece_b ^ (32 * (j % 2))) >= f.at.columns;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          rsrc, (__attribute__((address_space(3))) void*)(slot + (kBCopies * wave + j) * 512), 16,
+          (int)(out ? kOutOfRange : vb[j]), 0, 0, 0);
+    }
   }
 
-  template <int STAGES>
-  __device__ __forceinline__ void landed() const {
-    static_assert(STAGES * kCopies < 16, "vmcnt field");
+  // Waits until this wavefront's LDS reads are done and its copies but the last N have landed
+  // (unless they are known to have), then for the block.
+  template <int N>
+  __device__ __forceinline__ void meet(int& settled) const {
     asm volatile("" ::: "memory");  // no LDS access moves across the barrier
-    __builtin_amdgcn_s_waitcnt(0x0070 | (STAGES * kCopies));  // vmcnt, lgkmcnt(0)
+    if (settled > 0) {
+      --settled;
+      __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+    } else {
+      __builtin_amdgcn_s_waitcnt(0x0070 | N);  // vmcnt(N), lgkmcnt(0)
+    }
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   }
@@ -189,102 +219,135 @@ struct RowPipe {
     const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p + 4 * rows));
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
   }
-  __device__ __forceinline__ bf16x8 frag_a(const uint16_t* slot, int i) const {
-    if constexpr (AT) {
-      return across_frag(slot + a_line[i / 2] + 4 * (i % 2), kARows);
-    } else {
-      const int rows = HALVES ? (i / (AF / 2)) * (kARows / 2) + 32 * (i % (AF / 2) / 2) : 32 * (i / 2);
-      return *reinterpret_cast<const bf16x8*>(slot + a_at + (rows + 4 * (i % 2)) * 32);
-    }
-  }
-  __device__ __forceinline__ bf16x8 frag_b(const uint16_t* slot, int j) const {
-    if constexpr (BT)
-      return across_frag(slot + b_line[j], kBRows);
+  __device__ __forceinline__ bf16x8 frag_a(const uint16_t* slot, int kk, int i) const {
+    if constexpr (AT)
+      return across_frag(slot + a_line[i / 2] + kk * 32 * kHalf + 4 * (i % 2), kHalf);
     else
-      return *reinterpret_cast<const bf16x8*>(slot + b_at + 16 * j * 32);
+      return *reinterpret_cast<const bf16x8*>(slot + (a_at ^ (32 * kk)) + (32 * (i / 2) + 4 * (i % 2)) * kRowStage);
+  }
+  __device__ __forceinline__ bf16x8 frag_b(const uint16_t* slot, int kk, int j) const {
+    if constexpr (BT)
+      return across_frag(slot + b_line[j] + kk * 32 * kBRows, kBRows);
+    else
+      return *reinterpret_cast<const bf16x8*>(slot + (b_at ^ (32 * kk)) + 16 * j * kRowStage);
   }
 
-  template <int FIRST, int ROWS, int LATER, int COPIES>
+  // Keeps a step's order through scheduling: its reads and copies shared out among its products.
+  template <int READS, int COPIES>
   __device__ __forceinline__ void order() const {
-    __builtin_amdgcn_sched_group_barrier(0x100, FIRST, 0);
+    constexpr int kReads = (READS + BF - 1) / BF, kSome = (COPIES + BF - 1) / BF;
 #pragma unroll
     for (int j = 0; j < BF; ++j) {
-      __builtin_amdgcn_sched_group_barrier(0x008, ROWS, 0);
-      if (j < COPIES) __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
-      if constexpr (LATER > 0) __builtin_amdgcn_sched_group_barrier(0x100, LATER, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
+      if constexpr (kSome > 0) __builtin_amdgcn_sched_group_barrier(0x010, kSome, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, kH, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
   }
 
-  __device__ __forceinline__ void read_half0(const uint16_t* slot) {
-#pragma unroll
-    for (int i = 0; i < kH0; ++i) a0[i] = frag_a(slot, i);
-  }
-
-  __device__ __forceinline__ void half0(const uint16_t* cur) {
-#pragma unroll
-    for (int i = 0; i < kH1; ++i) a1[i] = frag_a(cur, kH0 + i);
+  __device__ __forceinline__ void multiply(int half, const bf16x8 (&a)[kH], const bf16x8 (&bb)[BF]) {
 #pragma unroll
     for (int j = 0; j < BF; ++j)
 #pragma unroll
-      for (int i = 0; i < kH0; ++i)
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0[i], b[j], acc[i][j], 0, 0, 0);
-    order<kH1 * kReadsA, kH0, 0, 0>();
+      for (int i = 0; i < kH; ++i)
+        acc[half * kH + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], bb[j], acc[half * kH + i][j], 0, 0, 0);
+  }
+  __device__ __forceinline__ void read_a(const uint16_t* slot, int kk, bf16x8 (&a)[kH]) const {
+#pragma unroll
+    for (int i = 0; i < kH; ++i) a[i] = frag_a(slot, kk, i);
+  }
+  __device__ __forceinline__ void read_b(const uint16_t* slot, int kk, bf16x8 (&bb)[BF]) const {
+#pragma unroll
+    for (int j = 0; j < BF; ++j) bb[j] = frag_b(slot, kk, j);
   }
 
-  __device__ __forceinline__ void half1(uint16_t* cur, const uint16_t* next, Stage at) {
-    landed<2>();
-    copy(cur, at);
-    read_half0(next);
-#pragma unroll
-    for (int j = 0; j < BF; ++j) {
-#pragma unroll
-      for (int i = 0; i < kH1; ++i)
-        acc[kH0 + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1[i], b[j], acc[kH0 + i][j], 0, 0, 0);
-      b[j] = frag_b(next, j);
-    }
-    order<kH0 * kReadsA, kH1, kReadsB, kCopies>();
-  }
-
-  // Stages q0 .. q1 of a contraction of nq_seg stages (`columns` columns) per segment; q_base: the
-  // stage at which the operands' pointers stand (0 where there are two segments).
-  __device__ __forceinline__ void contract(uint16_t* s0, uint16_t* s1, uint16_t* s2, uint16_t* s3, int q0, int q1,
-                                           int nq_seg, int64_t columns, int q_base) {
-    auto at = [&](int q) __attribute__((always_inline)) {
-      q = min(q, q1 - 1);
-      const bool second = q >= nq_seg;
-      const int in_seg = second ? q - nq_seg : q;
-      const int64_t left = columns - 32 * (int64_t)in_seg;
-      return Stage{in_seg - q_base, second, left < 32 ? (int)left : 32};
-    };
-    auto stage = [&](uint16_t* cur, uint16_t* next, int q) __attribute__((always_inline)) {
-      const Stage later = at(q + 4);
-      half0(cur);
-      half1(cur, next, later);
-    };
+  __device__ __forceinline__ void zero() {
 #pragma unroll
     for (int i = 0; i < AF; ++i)
 #pragma unroll
       for (int j = 0; j < BF; ++j) acc[i][j] = f32x4{};
-    copy(s0, at(q0));
-    copy(s1, at(q0 + 1));
-    copy(s2, at(q0 + 2));
-    copy(s3, at(q0 + 3));
-    landed<3>();
-    read_half0(s0);
-#pragma unroll
-    for (int j = 0; j < BF; ++j) b[j] = frag_b(s0, j);
-    int q = q0;
-    for (; q + 3 < q1; q += 4) {
-      stage(s0, s1, q);
-      stage(s1, s2, q + 1);
-      stage(s2, s3, q + 2);
-      stage(s3, s0, q + 3);
+  }
+
+  // Items index, index + stride, .. below count, one after the other: item(i) says where number i
+  // lies, done(i) takes its sums from acc.
+  template <typename Item, typename Done>
+  __device__ __forceinline__ void run(Slot s0, Slot s1, int index, int count, int stride, Item&& item, Done&& done) {
+    Feed f{item(index), index};
+    auto move = [&](int64_t a, int64_t b) __attribute__((always_inline)) {
+      f.at.a += a;
+      f.at.left_a -= a;
+      f.at.b += b;
+      f.at.left_b -= b;
+    };
+    auto advance = [&]() __attribute__((always_inline)) {
+      if (f.at.n > 1) {
+        --f.at.n;
+        ++f.at.first;
+        f.at.columns -= kRowStage;
+        move(k.step_a, k.step_b);
+        if (f.at.first == k.per_segment) {  // the second segment: its operands' bytes are counted anew
+          f.at.columns = k.columns;
+          f.at.a += k.jump_a;
+          f.at.left_a += (int64_t)k.per_segment * k.step_a;
+          f.at.b += k.jump_b;
+          f.at.left_b -= k.jump_b;
+        }
+      } else if (f.index + stride < count) {
+        f.index += stride;
+        f.at = item(f.index);
+      }  // else nothing follows: the last stage again
+    };
+    int pairs = f.at.n / 2, settled = 0;
+    auto stage = [&](Slot cur, Slot next) __attribute__((always_inline)) {
+      copy_a(next.a1, f, 1);
+      read_a(cur.a0, 1, ay);
+      read_b(cur.b, 1, b1);
+      multiply(0, ax, b0);
+      order<kH * kReadsA + BF * kReadsB, kACopies>();
+      meet<kCopies>(settled);  // X
+      advance();
+      copy_a(cur.a0, f, 0);
+      read_a(cur.a1, 0, ax);
+      multiply(0, ay, b1);
+      order<kH * kReadsA, kACopies>();
+      copy_b(cur.b, f, 0);
+      read_a(cur.a1, 1, ay);
+      multiply(1, ax, b0);
+      order<kH * kReadsA, kBCopies / 2>();
+      meet<kCopies - kBCopies / 2>(settled);  // Y
+      copy_b(cur.b, f, 1);
+      read_a(next.a0, 0, ax);
+      read_b(next.b, 0, b0);
+      multiply(1, ay, b1);
+      order<kH * kReadsA + BF * kReadsB, kBCopies / 2>();
+    };
+    copy_a(s0.a0, f, 0);
+    copy_b(s0.b, f, 0);
+    copy_b(s0.b, f, 1);
+    copy_a(s0.a1, f, 1);
+    advance();
+    copy_a(s1.a0, f, 0);
+    copy_b(s1.b, f, 0);
+    copy_b(s1.b, f, 1);
+    meet<kCopies>(settled);
+    read_a(s0.a0, 0, ax);
+    read_b(s0.b, 0, b0);
+    for (;;) {
+      zero();
+      for (int i = 0; i < pairs; ++i) {
+        stage(s0, s1);
+        stage(s1, s0);
+      }
+      // The copies in flight have landed before the results are written, so that the next two barriers
+      // need not wait for those.
+      __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+      settled = 2;
+      done(index);
+      index += stride;
+      if (index >= count) break;
+      pairs = item(index).n / 2;
     }
-    if (q < q1) stage(s0, s1, q);
-    if (q + 1 < q1) stage(s1, s2, q + 1);
-    if (q + 2 < q1) stage(s2, s3, q + 2);
-    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): nothing lands in LDS after the block is done
+    __builtin_amdgcn_s_waitcnt(0x0070);  // nothing lands in LDS after the block is done
     __syncthreads();
   }
 };
