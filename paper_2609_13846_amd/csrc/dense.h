@@ -81,6 +81,8 @@ size_t product_bytes(const Product& p);
 dtp_status launch_product(const Product& p, char* workspace, hipStream_t s);
 size_t product_bytes_bf16(const Product& p);  // dense_bf16.hip
 dtp_status launch_product_bf16(const Product& p, char* workspace, hipStream_t s);
+size_t product_bytes_f32(const Product& p);  // dense_f32.hip
+dtp_status launch_product_f32(const Product& p, char* workspace, hipStream_t s);
 
 #ifdef __HIPCC__
 

@@ -61,6 +61,12 @@ Workspace::~Workspace() {
   if (owned) (void)stream_free(owned, s);
 }
 
+size_t product_bytes(const Product& p) { return p.dtype == DTP_BF16 ? product_bytes_bf16(p) : product_bytes_f32(p); }
+
+dtp_status launch_product(const Product& p, char* workspace, hipStream_t s) {
+  return p.dtype == DTP_BF16 ? launch_product_bf16(p, workspace, s) : launch_product_f32(p, workspace, s);
+}
+
 namespace {
 
 // dz = scale act'(z) dy (linear), or dg = dh u act'(g) and du = dh act(g) (gated, `pre` [T][2][N]),

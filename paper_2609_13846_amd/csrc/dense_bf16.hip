@@ -2,12 +2,11 @@
 //
 //   tile_product_kernel    tiles through the LDS ring of row_gemm.h, the contraction split over
 //                          blocks where there are few tiles
-//   stream_product_kernel  few tokens: the weights streamed once, straight into registers
-//   join_product_kernel    the sum of a split contraction's parts, with the product's epilogue
+//   stream_product_kernel, join_product_kernel  few tokens, split contractions (dense_stream.h)
 //   pad_rows_kernel        copies of operands whose rows are not whole 16-byte pieces
 #include <algorithm>
 
-#include "dense.h"
+#include "dense_stream.h"
 #include "row_gemm.h"
 
 namespace dtp {
@@ -28,10 +27,11 @@ struct TileArgs {
   ProductOut out;
 };
 
-template <int W>
-__device__ __forceinline__ void store_partial(float* p, const float (&v)[W]) {
+// Kept pre-activations are read a whole pass later, from memory.
+__device__ __forceinline__ void store_kept(float* p, const float (&v)[8]) {
 #pragma unroll
-  for (int i = 0; i < W; i += 4) *reinterpret_cast<f32x4*>(p + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
+  for (int i = 0; i < 8; i += 4)
+    __builtin_nontemporal_store(f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]}, reinterpret_cast<f32x4*>(p + i));
 }
 
 __device__ __forceinline__ float half_of(const u32x4& v, int e) {
@@ -53,7 +53,7 @@ __device__ __forceinline__ void write_whole(const ProductOut& o, int64_t n, int 
   if constexpr (KIND == kProductLinear) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = c0[e] + half_of(bias, e);
-    if (o.pre) store_partial(o.pre + n * M + m, v);
+    if (o.pre) store_kept(o.pre + n * M + m, v);
     if (o.act != DTP_ACT_NONE) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = activate<uint16_t>(o.act, v[e]);
@@ -68,8 +68,8 @@ __device__ __forceinline__ void write_whole(const ProductOut& o, int64_t n, int 
     store_whole((uint16_t*)o.y + n * M + m, v);
   } else if constexpr (KIND == kProductGated) {
     if (o.pre) {
-      store_partial(o.pre + 2 * n * M + m, c0);
-      store_partial(o.pre + (2 * n + 1) * M + m, c1);
+      store_kept(o.pre + 2 * n * M + m, c0);
+      store_kept(o.pre + (2 * n + 1) * M + m, c1);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = activate<uint16_t>(o.act, c0[e]) * c1[e];
@@ -134,6 +134,7 @@ __global__ void __launch_bounds__(512, AF * BF > 16 ? 2 : 4) tile_product_kernel
       }
     };
     if (p.partial) {
+      pipe.settle();
       const int planes = kGated ? 2 : 1;
 #pragma unroll
       for (int j = 0; j < BF; ++j)
@@ -169,6 +170,7 @@ __global__ void __launch_bounds__(512, AF * BF > 16 ? 2 : 4) tile_product_kernel
 #pragma unroll
     for (int j = 0; j < BF; ++j) {
       if (j + 1 < BF) fetch(j + 1);
+      if (j == 0) pipe.settle();
 #pragma unroll
       for (int i = 0; i < kPairs; ++i) {
         const int n = n_lane + 16 * j, m = m_lane + 32 * i;
@@ -181,123 +183,6 @@ __global__ void __launch_bounds__(512, AF * BF > 16 ? 2 : 4) tile_product_kernel
   };
   const int items = tiles * ((p.nq + p.per - 1) / p.per);
   pipe.run({s0a0, s0a1, s0b}, {s1a0, s1a1, s1b}, blockIdx.x, items, gridDim.x, item, done);
-}
-
-// Few tokens (at most 16 TF): the time is that of reading the weights once.  A block takes 16
-// features (gated: 16 of each projection), its eight wavefronts deal out the columns in runs of
-// 64, and their sums meet in LDS.  Weights go straight into the matrix instruction's registers:
-// lane l reads 32 bytes of row l % 16, columns 16 (l / 16) of the run on, and the tokens' lanes
-// read the same columns, so any order of columns is as good as another.
-template <int TF, ProductKind KIND>
-__global__ void __launch_bounds__(512) stream_product_kernel(TileArgs p) {
-  constexpr bool kGated = KIND == kProductGated;
-  constexpr int kMats = kGated ? 2 : 1, kUnroll = TF > 1 ? 2 : 4;
-  __shared__ f32x4 sums[8][kMats * TF][64];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int r = lane % 16, g = lane / 16;
-  const int m0 = blockIdx.x * 16, m = min(m0 + r, p.M - 1);
-  const uint16_t* a[kMats];
-  a[0] = p.a0 + (int64_t)m * p.k.lda + 16 * g;
-  if constexpr (kGated) a[1] = p.a1 + (int64_t)m * p.k.lda + 16 * g;
-  const uint16_t* b[TF];
-#pragma unroll
-  for (int t = 0; t < TF; ++t) b[t] = p.b + (int64_t)min(16 * t + r, p.N - 1) * p.k.ldb + 16 * g;
-  f32x4 acc[kMats][TF] = {};
-  const int c0 = blockIdx.y * p.per, c1 = min(c0 + p.per, p.nq);  // runs
-  const int whole = min(c1, (int)(p.K / 64));
-  auto load = [](const uint16_t* q) { return *reinterpret_cast<const bf16x8*>(q); };
-  auto run = [&](auto n, int c) __attribute__((always_inline)) {
-    constexpr int N = decltype(n)::value;
-    bf16x8 fa[N][kMats][2], fb[N][TF][2];
-#pragma unroll
-    for (int u = 0; u < N; ++u) {
-      const int k = (c + 8 * u) * 64;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-#pragma unroll
-        for (int i = 0; i < kMats; ++i) fa[u][i][h] = load(a[i] + k + 8 * h);
-#pragma unroll
-        for (int t = 0; t < TF; ++t) fb[u][t][h] = load(b[t] + k + 8 * h);
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < N; ++u)
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int i = 0; i < kMats; ++i)
-#pragma unroll
-          for (int t = 0; t < TF; ++t)
-            acc[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[u][i][h], fb[u][t][h], acc[i][t], 0, 0, 0);
-  };
-  int c = c0 + wave;
-  for (; c + 8 * (kUnroll - 1) < whole; c += 8 * kUnroll) run(std::integral_constant<int, kUnroll>(), c);
-  for (; c < whole; c += 8) run(std::integral_constant<int, 1>(), c);
-  if (c < c1) {  // the run that the columns end in
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int k = c * 64 + 8 * h;
-      const bool in = k + 16 * g < p.K;
-      bf16x8 fa[kMats] = {};
-#pragma unroll
-      for (int i = 0; i < kMats; ++i)
-        if (in) fa[i] = load(a[i] + k);
-#pragma unroll
-      for (int t = 0; t < TF; ++t) {
-        bf16x8 fb = {};
-        if (in) fb = load(b[t] + k);
-#pragma unroll
-        for (int i = 0; i < kMats; ++i) acc[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[i], fb, acc[i][t], 0, 0, 0);
-      }
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < kMats; ++i)
-#pragma unroll
-    for (int t = 0; t < TF; ++t) sums[wave][i * TF + t][lane] = acc[i][t];
-  __syncthreads();
-  const int idx = threadIdx.x;
-  if (idx >= 32 * TF) return;
-  const int half = idx % 2, n = idx / 2, mm = m0 + 8 * half;
-  if (n >= p.N || mm >= p.M) return;
-  float v[2][8] = {};
-#pragma unroll
-  for (int i = 0; i < kMats; ++i)
-#pragma unroll
-    for (int w = 0; w < 8; ++w)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] += sums[w][i * TF + n / 16][(2 * half + e / 4) * 16 + n % 16][e % 4];
-  if (p.partial) {
-    float* at = p.partial + ((int64_t)blockIdx.y * kMats * p.N + n) * p.Mp + mm;
-    store_partial(at, v[0]);
-    if (kGated) store_partial(at + (int64_t)p.N * p.Mp, v[1]);
-  } else {
-    write_product<uint16_t, KIND, 8>(p.out, n, mm, p.M, v[0], v[1]);
-  }
-}
-
-template <ProductKind KIND>
-__global__ void __launch_bounds__(256) join_product_kernel(const float* __restrict__ partial, int splits, int M, int N,
-                                                           int Mp, ProductOut out) {
-  constexpr int kPlanes = KIND == kProductGated ? 2 : 1;
-  const int pieces = Mp / 8;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)N * pieces; i += (int64_t)gridDim.x * 256) {
-    const int64_t n = i / pieces;
-    const int m = (int)(i - n * pieces) * 8;
-    float v[2][8] = {};
-    for (int s = 0; s < splits; ++s)
-#pragma unroll
-      for (int pl = 0; pl < kPlanes; ++pl) {
-        const f32x4* at = reinterpret_cast<const f32x4*>(partial + (((int64_t)s * kPlanes + pl) * N + n) * Mp + m);
-        const f32x4 lo = at[0], hi = at[1];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          v[pl][e] += lo[e];
-          v[pl][4 + e] += hi[e];
-        }
-      }
-    write_product<uint16_t, KIND, 8>(out, n, m, M, v[0], v[1]);
-  }
 }
 
 // out[r][0 .. ld) = in[r][0 .. n), zeros behind.
@@ -325,13 +210,9 @@ struct Shape {
 Shape choose(const Product& p) {
   Shape s;
   const bool gated = p.kind == kProductGated;
-  if (!p.at && !p.bt && p.N <= 64) {
+  if (!p.at && !p.bt && p.N <= kStreamTokens) {
     s.stream = true;
-    s.nq = (int)((p.K + 63) / 64);
-    const int rows = (p.M + 15) / 16;
-    int splits = 1;
-    while (rows * splits < kCus / 2 && s.nq / (splits * 2) >= 16) splits *= 2;
-    s.per = (s.nq + splits - 1) / splits;
+    choose_stream<uint16_t>(p, s.nq, s.per);
   } else {
     s.nq = (int)((p.K + 2 * kRowStage - 1) / (2 * kRowStage)) * 2 * p.segments;
     auto tiles = [&](int t) { return ((int64_t)(gated ? 2 : 1) * p.M + t - 1) / t * ((p.N + t - 1) / t); };
@@ -391,24 +272,6 @@ void launch_tiles(TileArgs& t, const Shape& s, hipStream_t stream) {
     tile_product_kernel<4, 2, AT, BT, KIND><<<grid, 512, 0, stream>>>(t);
 }
 
-template <ProductKind KIND>
-void launch_stream(const TileArgs& t, const Shape& s, hipStream_t stream) {
-  const dim3 grid((t.M + 15) / 16, s.splits);
-  if (t.N <= 16)
-    stream_product_kernel<1, KIND><<<grid, 512, 0, stream>>>(t);
-  else if (t.N <= 32)
-    stream_product_kernel<2, KIND><<<grid, 512, 0, stream>>>(t);
-  else
-    stream_product_kernel<4, KIND><<<grid, 512, 0, stream>>>(t);
-}
-
-template <ProductKind KIND>
-void launch_join(const TileArgs& t, const Shape& s, hipStream_t stream) {
-  const int64_t threads = (int64_t)t.N * (t.Mp / 8);
-  join_product_kernel<KIND><<<(unsigned)std::min<int64_t>((threads + 255) / 256, 8192), 256, 0, stream>>>(
-      t.partial, s.splits, t.M, t.N, t.Mp, t.out);
-}
-
 }  // namespace
 
 size_t product_bytes_bf16(const Product& p) {
@@ -447,7 +310,8 @@ dtp_status launch_product_bf16(const Product& p, char* workspace, hipStream_t s)
   t.partial = uses_partial(p, shape) ? (float*)workspace : nullptr;
   t.out = p.out;
   if (shape.stream) {
-    p.kind == kProductGated ? launch_stream<kProductGated>(t, shape, s) : launch_stream<kProductLinear>(t, shape, s);
+    StreamArgs r{t.a0, t.a1, t.b, t.k.lda, t.k.ldb, t.M, t.N, t.Mp, p.K, shape.nq, shape.per, shape.splits, t.partial, t.out};
+    launch_stream<uint16_t>(p.kind, r, s);
   } else {
     t.m_tiles = (int)(((int64_t)(p.kind == kProductGated ? 2 : 1) * p.M + shape.tile - 1) / shape.tile);
     t.n_tiles = (int)((p.N + shape.tile - 1) / shape.tile);
@@ -463,11 +327,7 @@ dtp_status launch_product_bf16(const Product& p, char* workspace, hipStream_t s)
   }
   DTP_HIP(hipGetLastError());
   if (t.partial) {
-    switch (p.kind) {
-      case kProductLinear: launch_join<kProductLinear>(t, shape, s); break;
-      case kProductGated: launch_join<kProductGated>(t, shape, s); break;
-      case kProductGrad: launch_join<kProductGrad>(t, shape, s); break;
-    }
+    launch_join<uint16_t>(p.kind, t.partial, shape.splits, t.M, t.N, t.Mp, t.out, s);
     DTP_HIP(hipGetLastError());
   }
   return DTP_OK;

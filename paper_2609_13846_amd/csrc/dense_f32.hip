@@ -1,0 +1,278 @@
+// The fp32 products of the dense operators, on the fp32 matrix instructions: tiles of 128 x 128 (64 x
+// 64 where those would leave CUs idle), each wavefront a quarter of a tile in 32 x 32 pieces.
+//
+// An operand that lies along the contraction is kept [row][k] in LDS, so that a lane's 16-byte read
+// is the operand of four instructions; one that lies across it stays [k][row], a dword per
+// instruction.  Lane l feeds row l % 32 and, in step j of eight columns, column 4 (l / 32) + j, of
+// both operands alike.  The matrix cores need 64 cycles per instruction and 2 to 8 LDS reads
+// per eight instructions, so that loads through registers, one stage ahead, keep up.
+//
+// Sums of 256 columns are added to a total: the rounding of a long contraction grows with the length
+// of its runs, not with its own.
+#include <algorithm>
+
+#include "dense_stream.h"
+
+namespace dtp {
+namespace {
+
+constexpr int kCus = 256;
+constexpr int kStage = 16;                // columns per stage
+constexpr int kAlongRow = kStage + 4;     // floats: 16 rows' 16-byte reads cover the banks once
+constexpr int kFlush = 256 / kStage;      // stages between additions to the totals
+
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+
+struct TileArgs {
+  const float *a0, *a1, *b;
+  int64_t lda, ldb, K, b_seg;
+  int M, Mp, segments;
+  int64_t N;
+  int m_tiles, per, stages;  // stages per split, and of a segment
+  bool vec_a, vec_b;         // rows are whole 16-byte pieces
+  float* partial;
+  ProductOut out;
+};
+
+// One operand's stage on its way from memory to LDS: ROWS x 16 elements by 256 threads.
+template <int ROWS, bool ACROSS>
+struct Stage {
+  static constexpr int kPieces = ROWS * kStage / 4 / 256;
+  static constexpr int kAcrossRow = ROWS + 8;  // floats: lines 4 apart lie in the other half of the banks
+  static constexpr int kFloats = ACROSS ? kStage * kAcrossRow : ROWS * kAlongRow;
+  f32x4 v[kPieces];
+
+  __device__ __forceinline__ void load(const float* p, int64_t ld, bool vec, int64_t row0, int64_t rows, int64_t k0,
+                                       int64_t K) {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int at = threadIdx.x + 256 * i;
+      const int64_t row = row0 + (ACROSS ? at % (ROWS / 4) * 4 : at / 4), k = k0 + (ACROSS ? at / (ROWS / 4) : at % 4 * 4);
+      const int64_t along = ACROSS ? row : k, end = ACROSS ? rows : K;
+      const bool line = ACROSS ? k < K : row < rows;
+      const float* q = p + (ACROSS ? k * ld + row : row * ld + k);
+      v[i] = f32x4{};
+      if (line && along + 3 < end && vec) {
+        v[i] = *reinterpret_cast<const f32x4*>(q);
+      } else if (line) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (along + e < end) v[i][e] = q[e];
+      }
+    }
+  }
+  __device__ __forceinline__ void store(float* lds) const {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int at = threadIdx.x + 256 * i;
+      float* q = ACROSS ? lds + at / (ROWS / 4) * kAcrossRow + at % (ROWS / 4) * 4 : lds + at / 4 * kAlongRow + at % 4 * 4;
+      *reinterpret_cast<f32x4*>(q) = v[i];
+    }
+  }
+  // Columns 8 s + 4 (lane / 32) .. + 3 of row `row` + lane % 32.
+  __device__ __forceinline__ static f32x4 read(const float* lds, int row, int s, int lane) {
+    const int r = row + lane % 32, k = 8 * s + 4 * (lane / 32);
+    if constexpr (!ACROSS) return *reinterpret_cast<const f32x4*>(lds + r * kAlongRow + k);
+    f32x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = lds[(k + e) * kAcrossRow + r];
+    return v;
+  }
+};
+
+// F x F pieces of 32 x 32 per wavefront (gated: of each projection, F / 2 x F).
+template <int F, bool AT, bool BT, ProductKind KIND>
+__global__ void __launch_bounds__(256, 2) tile_product_f32_kernel(TileArgs p) {
+  constexpr bool kGated = KIND == kProductGated;
+  constexpr int kTile = 64 * F, kMats = kGated ? 2 : 1, kFM = kGated ? (F > 1 ? F / 2 : 1) : F;
+  constexpr int kRowsA = 64 * kFM;  // of each matrix
+  using SA = Stage<kRowsA, AT>;
+  using SB = Stage<kTile, BT>;
+  __shared__ __attribute__((aligned(16))) float lds[2][kMats * SA::kFloats + SB::kFloats];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int wm = wave & 1, wn = wave >> 1;
+  const int tm = blockIdx.x % p.m_tiles;
+  const int64_t m0 = (int64_t)tm * kRowsA, n0 = (int64_t)(blockIdx.x / p.m_tiles) * kTile;
+  const int q0 = blockIdx.y * p.per, q1 = min(q0 + p.per, p.stages * p.segments);
+  f32x16 acc[kMats][kFM][F] = {}, total[kMats][kFM][F] = {};
+  SA sa[kMats];
+  SB sb;
+  auto load = [&](int q) __attribute__((always_inline)) {
+    const int seg = q >= p.stages ? 1 : 0;
+    const int64_t k0 = (int64_t)(q - seg * p.stages) * kStage;
+#pragma unroll
+    for (int i = 0; i < kMats; ++i)
+      sa[i].load((kGated ? i : seg) ? p.a1 : p.a0, p.lda, p.vec_a, m0, p.M, k0, p.K);
+    sb.load(p.b + (BT ? 0 : seg * p.b_seg), p.ldb, p.vec_b, n0, p.N, k0, p.K);
+  };
+  auto store = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kMats; ++i) sa[i].store(lds[buf] + i * SA::kFloats);
+    sb.store(lds[buf] + kMats * SA::kFloats);
+  };
+  load(q0);
+  store(0);
+  __syncthreads();
+  int since = 0;
+  for (int q = q0; q < q1; ++q) {
+    const int buf = (q - q0) & 1;
+    if (q + 1 < q1) load(q + 1);
+#pragma unroll
+    for (int s = 0; s < kStage / 8; ++s) {
+      f32x4 a[kMats][kFM], b[F];
+#pragma unroll
+      for (int m = 0; m < kMats; ++m)
+#pragma unroll
+        for (int i = 0; i < kFM; ++i) a[m][i] = SA::read(lds[buf] + m * SA::kFloats, 32 * (wm * kFM + i), s, lane);
+#pragma unroll
+      for (int j = 0; j < F; ++j) b[j] = SB::read(lds[buf] + kMats * SA::kFloats, 32 * (wn * F + j), s, lane);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int m = 0; m < kMats; ++m)
+#pragma unroll
+          for (int i = 0; i < kFM; ++i)
+#pragma unroll
+            for (int j = 0; j < F; ++j)
+              acc[m][i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[m][i][e], b[j][e], acc[m][i][j], 0, 0, 0);
+    }
+    if (++since == kFlush) {
+      since = 0;
+#pragma unroll
+      for (int m = 0; m < kMats; ++m)
+#pragma unroll
+        for (int i = 0; i < kFM; ++i)
+#pragma unroll
+          for (int j = 0; j < F; ++j) {
+            total[m][i][j] += acc[m][i][j];
+            acc[m][i][j] = f32x16{};
+          }
+    }
+    if (q + 1 < q1) store(buf ^ 1);
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < kFM; ++i)
+#pragma unroll
+    for (int j = 0; j < F; ++j) {
+      const int64_t n = n0 + 32 * (wn * F + j) + lane % 32;
+      if (n >= p.N) continue;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int m = (int)m0 + 32 * (wm * kFM + i) + 8 * e + 4 * (lane / 32);
+        if (m >= p.M) continue;
+        float c[2][4] = {};
+#pragma unroll
+        for (int x = 0; x < kMats; ++x)
+#pragma unroll
+          for (int z = 0; z < 4; ++z) c[x][z] = acc[x][i][j][4 * e + z] + total[x][i][j][4 * e + z];
+        if (p.partial) {
+          float* at = p.partial + ((int64_t)blockIdx.y * kMats * p.N + n) * p.Mp + m;
+          store_partial(at, c[0]);
+          if (kGated) store_partial(at + p.N * p.Mp, c[1]);
+        } else {
+          write_product<float, KIND, 4>(p.out, n, m, p.M, c[0], c[1]);
+        }
+      }
+    }
+}
+
+struct Shape {
+  bool stream = false;
+  int f = 2, splits = 1, per = 0, stages = 0, m_tiles = 0;
+  int64_t n_tiles = 0;
+};
+
+Shape choose(const Product& p) {
+  Shape s;
+  const bool gated = p.kind == kProductGated;
+  if (!p.at && !p.bt && p.N <= 32 && p.lda % 4 == 0 && p.ldb % 4 == 0) {
+    s.stream = true;
+    choose_stream<float>(p, s.stages, s.per);
+    s.splits = (s.stages + s.per - 1) / s.per;
+    return s;
+  }
+  s.stages = (int)((p.K + kStage - 1) / kStage);
+  auto place = [&](int f) {
+    s.f = f;
+    const int rows = gated ? (f > 1 ? 32 * f : 64) : 64 * f;
+    s.m_tiles = (p.M + rows - 1) / rows;
+    s.n_tiles = (p.N + 64 * f - 1) / (64 * f);
+    return s.m_tiles * s.n_tiles;
+  };
+  int64_t tiles = place(2);
+  if (tiles < 2 * kCus) tiles = place(1);
+  const int64_t nq = (int64_t)s.stages * p.segments;
+  const int64_t want = (4 * kCus + tiles - 1) / tiles;
+  const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({tiles >= 2 * kCus ? 1 : want, nq / 8, 32}));
+  s.per = (int)((nq + splits - 1) / splits);
+  s.splits = (int)((nq + s.per - 1) / s.per);
+  return s;
+}
+
+size_t partial_bytes(const Product& p, const Shape& s) {
+  return s.splits == 1 ? 0
+                       : sizeof(float) * (size_t)s.splits * (p.kind == kProductGated ? 2 : 1) * (size_t)p.N *
+                             (size_t)((p.M + 7) / 8 * 8);
+}
+
+template <ProductKind KIND, bool AT, bool BT>
+void launch_tiles(const TileArgs& t, const Shape& s, hipStream_t stream) {
+  const dim3 grid((unsigned)(s.m_tiles * s.n_tiles), s.splits);
+  if (s.f == 2)
+    tile_product_f32_kernel<2, AT, BT, KIND><<<grid, 256, 0, stream>>>(t);
+  else
+    tile_product_f32_kernel<1, AT, BT, KIND><<<grid, 256, 0, stream>>>(t);
+}
+
+}  // namespace
+
+size_t product_bytes_f32(const Product& p) { return partial_bytes(p, choose(p)); }
+
+dtp_status launch_product_f32(const Product& p, char* workspace, hipStream_t s) {
+  const Shape shape = choose(p);
+  const int Mp = (p.M + 7) / 8 * 8;
+  float* partial = shape.splits > 1 ? (float*)workspace : nullptr;
+  if (shape.stream) {
+    const StreamArgs a{p.a0, p.a1, p.b, p.lda, p.ldb, p.M, (int)p.N, Mp, p.K, shape.stages, shape.per, shape.splits,
+                       partial, p.out};
+    launch_stream<float>(p.kind, a, s);
+  } else {
+    TileArgs t{};
+    t.a0 = (const float*)p.a0;
+    t.a1 = (const float*)p.a1;
+    t.b = (const float*)p.b;
+    t.lda = p.lda;
+    t.ldb = p.ldb;
+    t.K = p.K;
+    t.b_seg = p.b_seg;
+    t.M = p.M;
+    t.Mp = Mp;
+    t.segments = p.segments;
+    t.N = p.N;
+    t.m_tiles = shape.m_tiles;
+    t.per = shape.per;
+    t.stages = shape.stages;
+    t.vec_a = p.lda % 4 == 0;
+    t.vec_b = p.ldb % 4 == 0 && p.b_seg % 4 == 0;
+    t.partial = partial;
+    t.out = p.out;
+    switch (p.kind) {
+      case kProductLinear: launch_tiles<kProductLinear, false, false>(t, shape, s); break;
+      case kProductGated: launch_tiles<kProductGated, false, false>(t, shape, s); break;
+      case kProductGrad:
+        if (p.bt)
+          launch_tiles<kProductGrad, true, true>(t, shape, s);
+        else
+          launch_tiles<kProductGrad, true, false>(t, shape, s);
+    }
+  }
+  DTP_HIP(hipGetLastError());
+  if (partial) {
+    launch_join<float>(p.kind, partial, shape.splits, p.M, p.N, Mp, p.out, s);
+    DTP_HIP(hipGetLastError());
+  }
+  return DTP_OK;
+}
+
+}  // namespace dtp

@@ -1,0 +1,242 @@
+// Products of few tokens, and the sum of a split contraction's parts (bf16 and fp32).
+#pragma once
+
+#include <algorithm>
+
+#include "dense.h"
+
+namespace dtp {
+
+constexpr int kStreamTokens = 64;
+
+struct StreamArgs {
+  const void *a0, *a1, *b;
+  int64_t lda, ldb;
+  int M, N, Mp;    // Mp: M rounded up to 8, the row of a partial sum
+  int64_t K;
+  int runs, per;   // runs of columns in all, and per split
+  int splits;
+  float* partial;  // [splits][planes][N][Mp], or NULL
+  ProductOut out;
+};
+
+#ifdef __HIPCC__
+
+namespace {
+
+template <int W>
+__device__ __forceinline__ void store_partial(float* p, const float (&v)[W]) {
+#pragma unroll
+  for (int i = 0; i < W; i += 4) *reinterpret_cast<f32x4*>(p + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
+}
+
+// 16 bytes of a row, and the products of two of them: a lane's elements are of the same columns in
+// both operands, so that it does not matter which of the instruction's columns each is.
+template <typename S>
+struct Piece;
+template <>
+struct Piece<uint16_t> {
+  typedef bf16x8 V;
+  __device__ static __forceinline__ f32x4 multiply(const V& a, const V& b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+  }
+};
+template <>
+struct Piece<float> {
+  typedef f32x4 V;
+  __device__ static __forceinline__ f32x4 multiply(const V& a, const V& b, f32x4 c) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+    return c;
+  }
+};
+
+// At most 16 TF tokens: the time is that of reading the weights once.  A block takes 16 RF features
+// (gated: of each projection), its eight wavefronts deal out the columns in runs of 128 bytes a
+// row, and their sums meet in LDS.  Weights and tokens go straight into the matrix instruction's
+// registers: lane l reads 32 bytes of row l % 16, from byte 32 (l / 16) of the run on.  The loads
+// of the next group of runs are in flight while this one's are multiplied.
+template <typename S, int RF, int TF, ProductKind KIND>
+__global__ void __launch_bounds__(512, 4) stream_product_kernel(StreamArgs p) {
+  using P = Piece<S>;
+  using V = typename P::V;
+  constexpr bool kGated = KIND == kProductGated;
+  constexpr int kMats = kGated ? 2 : 1, kFrags = kMats * RF;
+  constexpr int kWide = 16 / sizeof(S), kRun = 8 * kWide;  // columns of a piece, and of a run
+  constexpr int kGroup = kFrags + TF > 3 ? 1 : 2;          // runs in flight beside those multiplied
+  __shared__ f32x4 sums[8][kFrags * TF][64];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int r = lane % 16, g = lane / 16;
+  const int m0 = blockIdx.x * 16 * RF;
+  const S *a[kFrags], *b[TF];
+#pragma unroll
+  for (int i = 0; i < kFrags; ++i) {
+    const int m = min(m0 + 16 * (i % RF) + r, p.M - 1);
+    a[i] = (const S*)(i / RF ? p.a1 : p.a0) + (int64_t)m * p.lda + 2 * kWide * g;
+  }
+#pragma unroll
+  for (int t = 0; t < TF; ++t) b[t] = (const S*)p.b + (int64_t)min(16 * t + r, p.N - 1) * p.ldb + 2 * kWide * g;
+  f32x4 acc[kFrags][TF] = {};
+  const int c0 = blockIdx.y * p.per, c1 = min(c0 + p.per, p.runs);
+  const int whole = min(c1, (int)(p.K / kRun));
+  V fa[2][kGroup][kFrags][2], fb[2][kGroup][TF][2];
+  auto fetch = [&](V (&xa)[kGroup][kFrags][2], V (&xb)[kGroup][TF][2], int c) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < kGroup; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int64_t k = (int64_t)(c + 8 * u) * kRun + kWide * h;
+#pragma unroll
+        for (int i = 0; i < kFrags; ++i) xa[u][i][h] = *reinterpret_cast<const V*>(a[i] + k);
+#pragma unroll
+        for (int t = 0; t < TF; ++t) xb[u][t][h] = *reinterpret_cast<const V*>(b[t] + k);
+      }
+  };
+  auto multiply = [&](const V (&xa)[kGroup][kFrags][2], const V (&xb)[kGroup][TF][2]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < kGroup; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < kFrags; ++i)
+#pragma unroll
+          for (int t = 0; t < TF; ++t) acc[i][t] = P::multiply(xa[u][i][h], xb[u][t][h], acc[i][t]);
+  };
+  constexpr int kStep = 8 * kGroup;  // runs a group of all wavefronts covers
+  int c = c0 + wave;
+  // groups of this wavefront that are whole: runs c + 8 u < whole
+  const int groups = max(0, (whole - c + 7) / 8 / kGroup);
+  if (groups > 0) fetch(fa[0], fb[0], c);
+  for (int q = 0; q < groups; q += 2) {
+    if (q + 1 < groups) fetch(fa[1], fb[1], c + kStep);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(fa[0], fb[0]);
+    if (q + 1 >= groups) break;
+    if (q + 2 < groups) fetch(fa[0], fb[0], c + 2 * kStep);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(fa[1], fb[1]);
+    c += 2 * kStep;
+  }
+  c = c0 + wave + groups * kStep;
+  for (; c < c1; c += 8)  // single runs, and the one that the columns end in
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int64_t k = (int64_t)c * kRun + kWide * h;
+      const bool in = k + 2 * kWide * g < p.K;
+      V xa[kFrags] = {};
+#pragma unroll
+      for (int i = 0; i < kFrags; ++i)
+        if (in) xa[i] = *reinterpret_cast<const V*>(a[i] + k);
+#pragma unroll
+      for (int t = 0; t < TF; ++t) {
+        V xb = {};
+        if (in) xb = *reinterpret_cast<const V*>(b[t] + k);
+#pragma unroll
+        for (int i = 0; i < kFrags; ++i) acc[i][t] = P::multiply(xa[i], xb, acc[i][t]);
+      }
+    }
+#pragma unroll
+  for (int i = 0; i < kFrags; ++i)
+#pragma unroll
+    for (int t = 0; t < TF; ++t) sums[wave][i * TF + t][lane] = acc[i][t];
+  __syncthreads();
+  // a thread per W features of a token; lane 16 (m / 4) + n of a fragment holds rows m .. m + 3
+  constexpr int W = Elem<S>::kWide, kPieces = 16 * RF / W;
+  for (int idx = threadIdx.x; idx < 16 * TF * kPieces; idx += 512) {
+    const int n = idx / kPieces, row = idx % kPieces * W, mm = m0 + row;
+    if (n >= p.N || mm >= p.M) continue;
+    float v[2][W] = {};
+#pragma unroll
+    for (int i = 0; i < kMats; ++i)
+#pragma unroll
+      for (int w = 0; w < 8; ++w)
+#pragma unroll
+        for (int e = 0; e < W; e += 4) {
+          const f32x4 x = sums[w][(i * RF + row / 16) * TF + n / 16][(row % 16 + e) / 4 * 16 + n % 16];
+#pragma unroll
+          for (int z = 0; z < 4; ++z) v[i][e + z] += x[z];
+        }
+    if (p.partial) {
+      float* at = p.partial + ((int64_t)blockIdx.y * kMats * p.N + n) * p.Mp + mm;
+      store_partial(at, v[0]);
+      if (kGated) store_partial(at + (int64_t)p.N * p.Mp, v[1]);
+    } else {
+      write_product<S, KIND, W>(p.out, n, mm, p.M, v[0], v[1]);
+    }
+  }
+}
+
+// The sums of a split contraction's parts, in order.
+template <typename S, ProductKind KIND>
+__global__ void __launch_bounds__(256) join_product_kernel(const float* __restrict__ partial, int splits, int M, int64_t N,
+                                                           int Mp, ProductOut out) {
+  constexpr int kPlanes = KIND == kProductGated ? 2 : 1, W = Elem<S>::kWide;
+  const int pieces = Mp / W;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < N * pieces; i += (int64_t)gridDim.x * 256) {
+    const int64_t n = i / pieces;
+    const int m = (int)(i - n * pieces) * W;
+    float v[2][W] = {};
+    for (int s = 0; s < splits; ++s)
+#pragma unroll
+      for (int pl = 0; pl < kPlanes; ++pl) {
+        const f32x4* at = reinterpret_cast<const f32x4*>(partial + (((int64_t)s * kPlanes + pl) * N + n) * Mp + m);
+#pragma unroll
+        for (int e = 0; e < W; e += 4) {
+          const f32x4 x = at[e / 4];
+#pragma unroll
+          for (int z = 0; z < 4; ++z) v[pl][e + z] += x[z];
+        }
+      }
+    write_product<S, KIND, W>(out, n, m, M, v[0], v[1]);
+  }
+}
+
+// Runs of a few-token product, and how many a block takes: the contraction is split where the
+// features alone would leave CUs idle and every wavefront keeps at least four runs.
+template <typename S>
+void choose_stream(const Product& p, int& runs, int& per) {
+  runs = (int)((p.K * (int64_t)sizeof(S) + 127) / 128);
+  const int blocks = (p.M + 15) / 16;
+  int splits = 1;
+  while (blocks * splits < 128 && runs / (splits * 2) >= 32) splits *= 2;
+  per = (runs + splits - 1) / splits;
+}
+
+template <typename S, ProductKind KIND>
+void launch_stream_kind(const StreamArgs& a, hipStream_t s) {
+  // Tokens' pieces are read once per block: two feature fragments share them where there are many.
+  const dim3 one((a.M + 15) / 16, a.splits), two((a.M + 31) / 32, a.splits);
+  if (a.N <= 16)
+    stream_product_kernel<S, 1, 1, KIND><<<one, 512, 0, s>>>(a);
+  else if (a.N <= 32)
+    stream_product_kernel<S, 1, 2, KIND><<<one, 512, 0, s>>>(a);
+  else
+    stream_product_kernel<S, 1, 4, KIND><<<one, 512, 0, s>>>(a);
+  (void)two;
+}
+
+template <typename S>
+void launch_stream(ProductKind kind, const StreamArgs& a, hipStream_t s) {
+  if (kind == kProductGated)
+    launch_stream_kind<S, kProductGated>(a, s);
+  else
+    launch_stream_kind<S, kProductLinear>(a, s);
+}
+
+template <typename S>
+void launch_join(ProductKind kind, const float* partial, int splits, int M, int64_t N, int Mp, const ProductOut& out,
+                 hipStream_t s) {
+  const unsigned blocks = (unsigned)std::min<int64_t>((N * (Mp / Elem<S>::kWide) + 255) / 256, 8192);
+  if (kind == kProductLinear)
+    join_product_kernel<S, kProductLinear><<<blocks, 256, 0, s>>>(partial, splits, M, N, Mp, out);
+  else if (kind == kProductGated)
+    join_product_kernel<S, kProductGated><<<blocks, 256, 0, s>>>(partial, splits, M, N, Mp, out);
+  else
+    join_product_kernel<S, kProductGrad><<<blocks, 256, 0, s>>>(partial, splits, M, N, Mp, out);
+}
+
+}  // namespace
+
+#endif  // __HIPCC__
+
+}  // namespace dtp

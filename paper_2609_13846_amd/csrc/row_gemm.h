@@ -238,9 +238,10 @@ struct RowPipe {
     constexpr int kReads = (READS + BF - 1) / BF, kSome = (COPIES + BF - 1) / BF;
 #pragma unroll
     for (int j = 0; j < BF; ++j) {
-      __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
       if constexpr (kSome > 0) __builtin_amdgcn_sched_group_barrier(0x010, kSome, 0);
-      __builtin_amdgcn_sched_group_barrier(0x008, kH, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, kH - 1, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
   }
@@ -259,6 +260,14 @@ struct RowPipe {
   __device__ __forceinline__ void read_b(const uint16_t* slot, int kk, bf16x8 (&bb)[BF]) const {
 #pragma unroll
     for (int j = 0; j < BF; ++j) bb[j] = frag_b(slot, kk, j);
+  }
+
+  // Waits for the copies in flight: before a result is written, so that the next two barriers need not
+  // wait for the writes.
+  __device__ __forceinline__ static void settle() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+    asm volatile("" ::: "memory");
   }
 
   __device__ __forceinline__ void zero() {
@@ -338,10 +347,7 @@ struct RowPipe {
         stage(s0, s1);
         stage(s1, s0);
       }
-      // The copies in flight have landed before the results are written, so that the next two barriers
-      // need not wait for those.
-      __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
-      settled = 2;
+      settled = 2;  // done() waits for the copies in flight
       done(index);
       index += stride;
       if (index >= count) break;
