@@ -33,7 +33,6 @@ struct ProductOut {
   int act = DTP_ACT_NONE;
   int64_t n_split = INT64_MAX;  // gradient rows: [0, n_keep) to y, n_split + [0, n_keep) to y2
   int64_t n_keep = INT64_MAX;
-  bool vec = false;  // M is a multiple of 8, so that groups of 8 (bf16) or 4 (fp32) are 16 bytes aligned
 };
 
 struct Product {
@@ -146,15 +145,21 @@ __device__ __forceinline__ void activate_grad(int act, float z, float& a, float&
   a = z * s;
 }
 
+// 16 bytes at any address of the element type's alignment: global memory takes such loads and stores
+// whole, so that rows of odd lengths need no path of their own.
+typedef u32x4 __attribute__((aligned(2))) u32x4_any;
+typedef f32x4 __attribute__((aligned(4))) f32x4_any;
+
+// W elements of a row, or the `count` that are left of it.
 template <typename S, int W>
-__device__ __forceinline__ void load_row(const S* p, bool vec, int count, float (&v)[W]) {
-  if (vec) {
+__device__ __forceinline__ void load_row(const S* p, int count, float (&v)[W]) {
+  if (count >= W) {
     union {
       u32x4 q[W * sizeof(S) / 16];
       S e[W];
     } u;
 #pragma unroll
-    for (int i = 0; i < (int)(W * sizeof(S) / 16); ++i) u.q[i] = reinterpret_cast<const u32x4*>(p)[i];
+    for (int i = 0; i < (int)(W * sizeof(S) / 16); ++i) u.q[i] = reinterpret_cast<const u32x4_any*>(p)[i];
 #pragma unroll
     for (int i = 0; i < W; ++i) v[i] = Elem<S>::load(u.e[i]);
   } else {
@@ -164,16 +169,22 @@ __device__ __forceinline__ void load_row(const S* p, bool vec, int count, float 
 }
 
 template <typename S, int W>
-__device__ __forceinline__ void store_row(S* p, bool vec, int count, const float (&v)[W]) {
-  if (vec) {
+__device__ __forceinline__ void store_row(S* p, int count, const float (&v)[W]) {
+  if (count >= W) {
     union {
       u32x4 q[W * sizeof(S) / 16];
-      S e[W];
+      uint32_t d[W * sizeof(S) / 4];
+      float f[W * sizeof(S) / 4];
     } u;
+    if constexpr (sizeof(S) == 2) {
 #pragma unroll
-    for (int i = 0; i < W; ++i) u.e[i] = Elem<S>::store(v[i]);
+      for (int i = 0; i < W / 2; ++i) u.d[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+    } else {
 #pragma unroll
-    for (int i = 0; i < (int)(W * sizeof(S) / 16); ++i) reinterpret_cast<u32x4*>(p)[i] = u.q[i];
+      for (int i = 0; i < W; ++i) u.f[i] = v[i];
+    }
+#pragma unroll
+    for (int i = 0; i < (int)(W * sizeof(S) / 16); ++i) reinterpret_cast<u32x4_any*>(p)[i] = u.q[i];
   } else {
 #pragma unroll
     for (int i = 0; i < W; ++i)
@@ -194,40 +205,41 @@ __device__ __forceinline__ void write_product(const ProductOut& o, int64_t n, in
     for (int i = 0; i < W; ++i) v[i] = c0[i];
     if (o.bias) {
       float b[W];
-      load_row((const S*)o.bias + m, o.vec, count, b);
+      load_row((const S*)o.bias + m, count, b);
 #pragma unroll
       for (int i = 0; i < W; ++i) v[i] += b[i];
     }
-    if (o.pre) store_row(o.pre + n * M + m, o.vec, count, v);
+    if (o.pre) store_row(o.pre + n * M + m, count, v);
     if (o.act != DTP_ACT_NONE) {
 #pragma unroll
       for (int i = 0; i < W; ++i) v[i] = activate<S>(o.act, v[i]);
     }
     if (o.residual) {
       float r[W];
-      load_row((const S*)o.residual + n * M + m, o.vec, count, r);
+      load_row((const S*)o.residual + n * M + m, count, r);
 #pragma unroll
       for (int i = 0; i < W; ++i) v[i] = fmaf(o.alpha, v[i], r[i]);
     } else {
 #pragma unroll
       for (int i = 0; i < W; ++i) v[i] *= o.alpha;
     }
-    store_row((S*)o.y + n * M + m, o.vec, count, v);
+    store_row((S*)o.y + n * M + m, count, v);
   } else if constexpr (KIND == kProductGated) {
     if (o.pre) {
-      store_row(o.pre + 2 * n * M + m, o.vec, count, c0);
-      store_row(o.pre + (2 * n + 1) * M + m, o.vec, count, c1);
+      store_row(o.pre + 2 * n * M + m, count, c0);
+      store_row(o.pre + (2 * n + 1) * M + m, count, c1);
     }
 #pragma unroll
     for (int i = 0; i < W; ++i) v[i] = activate<S>(o.act, c0[i]) * c1[i];
-    store_row((S*)o.y + n * M + m, o.vec, count, v);
+    store_row((S*)o.y + n * M + m, count, v);
   } else {
     const bool second = n >= o.n_split;
     const int64_t row = second ? n - o.n_split : n;
     if (row >= o.n_keep) return;
 #pragma unroll
     for (int i = 0; i < W; ++i) v[i] = o.alpha * c0[i];
-    store_row((S*)(second ? o.y2 : o.y) + row * M + m, o.vec, count, v);
+    S *const y1 = (S*)o.y, *const y2 = (S*)o.y2;
+    store_row((second ? y2 : y1) + row * M + m, count, v);
   }
 }
 

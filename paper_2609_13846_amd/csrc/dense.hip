@@ -75,7 +75,7 @@ namespace {
 template <typename S, bool GATED>
 __global__ void __launch_bounds__(256)
 activation_grad_kernel(const S* __restrict__ dy, const float* __restrict__ pre, int act, float scale, int64_t T, int N,
-                       int ld, bool vec, S* __restrict__ dz) {
+                       int ld, S* __restrict__ dz) {
   constexpr int W = Elem<S>::kWide;
   const int pieces = ld / W;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < T * pieces; i += (int64_t)gridDim.x * 256) {
@@ -83,9 +83,9 @@ activation_grad_kernel(const S* __restrict__ dy, const float* __restrict__ pre, 
     const int n = (int)(i - t * pieces) * W, count = N - n;
     float g[W] = {}, u[W] = {}, d[W] = {};
     if (count > 0) {
-      load_row(dy + t * N + n, vec, count, d);
-      if (pre) load_row(pre + (GATED ? 2 : 1) * t * N + n, vec, count, g);
-      if (GATED) load_row(pre + (2 * t + 1) * N + n, vec, count, u);
+      load_row(dy + t * N + n, count, d);
+      if (pre) load_row(pre + (GATED ? 2 : 1) * t * N + n, count, g);
+      if (GATED) load_row(pre + (2 * t + 1) * N + n, count, u);
     }
 #pragma unroll
     for (int e = 0; e < W; ++e) {
@@ -100,8 +100,8 @@ activation_grad_kernel(const S* __restrict__ dy, const float* __restrict__ pre, 
       }
     }
     S* out = dz + t * (GATED ? 2 : 1) * ld + n;
-    store_row(out, true, W, g);
-    if (GATED) store_row(out + ld, true, W, u);
+    store_row(out, W, g);
+    if (GATED) store_row(out + ld, W, u);
   }
 }
 
@@ -112,7 +112,7 @@ constexpr int kSumCols = 256;
 template <typename S>
 __global__ void __launch_bounds__(256)
 column_sums_kernel(const S* __restrict__ dy, const float* __restrict__ pre, int act, float scale, int64_t T, int N,
-                   int64_t rows, bool vec, float* __restrict__ partial) {
+                   int64_t rows, float* __restrict__ partial) {
   __shared__ float sums[8][kSumCols];
   const int group = threadIdx.x % 32, lane = threadIdx.x / 32;
   const int n = blockIdx.x * kSumCols + 8 * group, count = N - n;
@@ -121,8 +121,8 @@ column_sums_kernel(const S* __restrict__ dy, const float* __restrict__ pre, int 
   if (count > 0)
     for (int64_t t = t0 + lane; t < t1; t += 8) {
       float d[8], z[8];
-      load_row(dy + t * N + n, vec, count, d);
-      if (act != DTP_ACT_NONE) load_row(pre + t * N + n, vec, count, z);
+      load_row(dy + t * N + n, count, d);
+      if (act != DTP_ACT_NONE) load_row(pre + t * N + n, count, z);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         float a, da = 1.0f;
@@ -141,13 +141,22 @@ column_sums_kernel(const S* __restrict__ dy, const float* __restrict__ pre, int 
   partial[(int64_t)blockIdx.y * N + col] = v;
 }
 
+// A block: 32 columns, their chunks dealt to eight threads each and summed in 64 bits.
 template <typename S>
 __global__ void __launch_bounds__(256)
 join_sums_kernel(const float* __restrict__ partial, int chunks, int N, S* __restrict__ out) {
-  const int n = blockIdx.x * 256 + threadIdx.x;
-  if (n >= N) return;
+  __shared__ double sums[8][32];
+  const int col = threadIdx.x % 32, lane = threadIdx.x / 32, n = blockIdx.x * 32 + col;
   double v = 0.0;
-  for (int c = 0; c < chunks; ++c) v += (double)partial[(int64_t)c * N + n];
+  if (n < N) {
+#pragma unroll 8
+    for (int c = lane; c < chunks; c += 8) v += (double)partial[(int64_t)c * N + n];
+  }
+  sums[lane][col] = v;
+  __syncthreads();
+  if (lane != 0 || n >= N) return;
+#pragma unroll
+  for (int l = 1; l < 8; ++l) v += sums[l][col];
   out[n] = Elem<S>::store((float)v);
 }
 
@@ -178,13 +187,13 @@ dtp_status launch_column_sums(const void* dy, const float* pre, int act, float s
   const int chunks = (int)sum_chunks(T);
   const dim3 grid((N + kSumCols - 1) / kSumCols, chunks);
   if (dtype == DTP_BF16) {
-    column_sums_kernel<<<grid, 256, 0, s>>>((const uint16_t*)dy, pre, act, scale, T, N, sum_chunk_rows(T), N % 8 == 0,
+    column_sums_kernel<<<grid, 256, 0, s>>>((const uint16_t*)dy, pre, act, scale, T, N, sum_chunk_rows(T), 
                                             partial);
-    join_sums_kernel<<<(N + 255) / 256, 256, 0, s>>>(partial, chunks, N, (uint16_t*)out);
+    join_sums_kernel<<<(N + 31) / 32, 256, 0, s>>>(partial, chunks, N, (uint16_t*)out);
   } else {
-    column_sums_kernel<<<grid, 256, 0, s>>>((const float*)dy, pre, act, scale, T, N, sum_chunk_rows(T), N % 8 == 0,
+    column_sums_kernel<<<grid, 256, 0, s>>>((const float*)dy, pre, act, scale, T, N, sum_chunk_rows(T), 
                                             partial);
-    join_sums_kernel<<<(N + 255) / 256, 256, 0, s>>>(partial, chunks, N, (float*)out);
+    join_sums_kernel<<<(N + 31) / 32, 256, 0, s>>>(partial, chunks, N, (float*)out);
   }
   DTP_HIP(hipGetLastError());
   return DTP_OK;
@@ -195,10 +204,10 @@ dtp_status launch_activation_grad(const void* dy, const float* pre, int act, flo
                                   int dtype, void* dz, hipStream_t s) {
   if (dtype == DTP_BF16)
     activation_grad_kernel<uint16_t, GATED><<<blocks_of(T * (ld / 8)), 256, 0, s>>>(
-        (const uint16_t*)dy, pre, act, scale, T, N, ld, N % 8 == 0, (uint16_t*)dz);
+        (const uint16_t*)dy, pre, act, scale, T, N, ld,  (uint16_t*)dz);
   else
     activation_grad_kernel<float, GATED><<<blocks_of(T * (ld / 4)), 256, 0, s>>>(
-        (const float*)dy, pre, act, scale, T, N, ld, N % 8 == 0, (float*)dz);
+        (const float*)dy, pre, act, scale, T, N, ld,  (float*)dz);
   DTP_HIP(hipGetLastError());
   return DTP_OK;
 }
@@ -222,7 +231,6 @@ Product forward_product(ProductKind kind, int64_t T, int K, int N, int dtype) {
   p.M = N;
   p.N = T;
   p.K = K;
-  p.out.vec = N % 8 == 0;
   return p;
 }
 
@@ -239,7 +247,6 @@ Product dx_product(int64_t T, int K, int N, int parts, int ld, int dtype) {
   p.K = N;
   p.segments = parts;
   p.b_seg = ld;
-  p.out.vec = K % 8 == 0;
   return p;
 }
 
@@ -257,7 +264,6 @@ Product dw_product(int64_t T, int K, int N, int parts, int ld, int dtype) {
     p.out.n_split = ld;
     p.out.n_keep = N;
   }
-  p.out.vec = K % 8 == 0;
   return p;
 }
 

@@ -31,7 +31,7 @@ struct TileArgs {
 __device__ __forceinline__ void store_kept(float* p, const float (&v)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; i += 4)
-    __builtin_nontemporal_store(f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]}, reinterpret_cast<f32x4*>(p + i));
+    __builtin_nontemporal_store(f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]}, reinterpret_cast<f32x4_any*>(p + i));
 }
 
 __device__ __forceinline__ float half_of(const u32x4& v, int e) {
@@ -41,7 +41,7 @@ __device__ __forceinline__ void store_whole(uint16_t* p, const float (&v)[8]) {
   u32x4 o;
 #pragma unroll
   for (int e = 0; e < 4; ++e) o[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
-  *reinterpret_cast<u32x4*>(p) = o;
+  *reinterpret_cast<u32x4_any*>(p) = o;
 }
 
 // write_product for eight whole, aligned features.
@@ -85,9 +85,11 @@ __device__ __forceinline__ void write_whole(const ProductOut& o, int64_t n, int 
   }
 }
 
-// One block per CU (256 x 256 tiles; two of 128 x 128), each with a run of items: a tile, or a split of
+// One block per CU (256 x 256 tiles; two of 128 x 128, three of 128 x 64), each with a run of items: a tile, or a split of
 // its contraction.  Items are numbered so that the ones that run together on an XCD share operands.
-template <int AF, int BF, bool AT, bool BT, ProductKind KIND>
+// ENDS: M need not be a multiple of 8.  (A kernel of its own for the linear epilogue, whose registers
+// the path for rows' ends would spill: 735 -> 829 us for 65,536 x 1,024 x 6,144.)
+template <int AF, int BF, bool AT, bool BT, ProductKind KIND, bool ENDS>
 __global__ void __launch_bounds__(512, AF * BF > 16 ? 2 : 4) tile_product_kernel(TileArgs p) {
   constexpr bool kGated = KIND == kProductGated;
   using Pipe = RowPipe<AF, BF, AT, BT, kGated>;
@@ -150,6 +152,19 @@ __global__ void __launch_bounds__(512, AF * BF > 16 ? 2 : 4) tile_product_kernel
         }
       return;
     }
+    if (ENDS && p.M % 8 != 0 && m0 + kTileM > p.M) {  // rows that end inside a lane's eight
+      pipe.settle();
+#pragma unroll
+      for (int j = 0; j < BF; ++j)
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) {
+          if (n_lane + 16 * j >= p.N) continue;
+          float c0[8], c1[8];
+          sums(i, j, c0, c1);
+          write_product<uint16_t, KIND, 8>(p.out, n_lane + 16 * j, m_lane + 32 * i, p.M, c0, c1);
+        }
+      return;
+    }
     // results a row at a time, the next row's residual on its way beside this one's writes
     constexpr bool kLinear = KIND == kProductLinear;
     u32x4 bias[kPairs] = {}, residual[2][kPairs] = {};
@@ -163,7 +178,7 @@ __global__ void __launch_bounds__(512, AF * BF > 16 ? 2 : 4) tile_product_kernel
 #pragma unroll
       for (int i = 0; i < kPairs; ++i)
         if (m_lane + 32 * i < p.M)
-          residual[j % 2][i] = *reinterpret_cast<const u32x4*>((const uint16_t*)p.out.residual +
+          residual[j % 2][i] = *reinterpret_cast<const u32x4_any*>((const uint16_t*)p.out.residual +
                                                                (int64_t)(n_lane + 16 * j) * p.M + m_lane + 32 * i);
     };
     fetch(0);
@@ -203,26 +218,64 @@ __global__ void __launch_bounds__(256) pad_rows_kernel(const uint16_t* __restric
 // ---------------------------------------------------------------------------- plan
 struct Shape {
   bool stream = false;
-  int tile = 256;      // rows and columns of a tile
+  int tile = 0;        // of kTiles
   int splits = 1, per = 0, nq = 0;
 };
+
+// The tile and the splits of the contraction by the launch's estimated length in us: a CU's items, one
+// stage of 64 columns after the other, half of the operands' bytes at memory speed (the other half is
+// read beside the products), and the join of the parts.  Measured (T x K x N, the best of all tiles and splits against the choice): 64 x 14,336 x
+// 4,096 26.3, 26.3; 777 x 1,040 x 2,816 13.8, 13.8; dW of 16,384 x 4,096 x 1,536 184, 184 (128 x 128:
+// 234).
+struct Tile {
+  int m, n;        // rows of A and of B
+  int per_cu;      // blocks of a CU
+  double alone, shared;  // us per stage: one item per CU, several
+  double item;     // us per item beside its stages: results, the first copies
+};
+constexpr Tile kTiles[] = {{256, 256, 1, 1.28, 1.32, 5.0}, {128, 128, 2, 0.50, 0.49, 1.0}, {128, 64, 3, 0.39, 0.33, 0.8}};
+
+// Up to 8 tokens the weights are streamed into registers, and up to 16 where they are few: each block
+// reads the tokens too, as many bytes as of weights at 16 tokens (14,336 x 4,096: 24 us for one token,
+// 31 for 16 and 27 in tiles; 4,096 x 4,096: 10 and 12.5).
+bool streams(const Product& p) {
+  if (p.at || p.bt) return false;
+  return p.N <= 8 || (p.N <= kStreamTokens && (int64_t)p.M * p.K <= ((int64_t)1 << 24));
+}
 
 Shape choose(const Product& p) {
   Shape s;
   const bool gated = p.kind == kProductGated;
-  if (!p.at && !p.bt && p.N <= kStreamTokens) {
+  if (streams(p)) {
     s.stream = true;
     choose_stream<uint16_t>(p, s.nq, s.per);
-  } else {
-    s.nq = (int)((p.K + 2 * kRowStage - 1) / (2 * kRowStage)) * 2 * p.segments;
-    auto tiles = [&](int t) { return ((int64_t)(gated ? 2 : 1) * p.M + t - 1) / t * ((p.N + t - 1) / t); };
-    s.tile = tiles(256) >= 192 ? 256 : 128;
-    if (p.bt && tiles(256) * (s.nq / 8) >= 192) s.tile = 256;
-    const int64_t n = tiles(s.tile), room = s.tile == 256 ? kCus : 2 * kCus;
-    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({n >= room / 2 && !p.bt ? 1 : (3 * room + n - 1) / n, s.nq / 4, 16}));
-    s.per = (int)((s.nq / 2 + splits - 1) / splits) * 2;
+    s.splits = (s.nq + s.per - 1) / s.per;
+    return s;
   }
-  s.splits = (s.nq + s.per - 1) / s.per;
+  // every item has an even number of stages
+  s.nq = (int)((p.K + 2 * kRowStage - 1) / (2 * kRowStage)) * 2 * p.segments;
+  const double M = (gated ? 2.0 : 1.0) * p.M, N = (double)p.N;
+  const double stream = 2.0 * (M + N) * (double)p.K * p.segments / 5.5e6;  // us at 5.5 TB/s
+  double best = 1e30;
+  for (int i = 0; i < 3; ++i) {
+    const Tile& t = kTiles[i];
+    const int64_t tiles = (((int64_t)M + t.m - 1) / t.m) * ((p.N + t.n - 1) / t.n);
+    for (int splits = 1; splits <= std::min(32, s.nq / 2); ++splits) {
+      const int per = (s.nq / 2 + splits - 1) / splits * 2;
+      const int real = (s.nq + per - 1) / per;
+      if (real != splits) continue;
+      const int64_t items = (tiles * splits + kCus - 1) / kCus;  // of a CU
+      double us = (double)items * (per * (items > 1 ? t.shared : t.alone) + t.item);
+      us += 0.5 * stream;
+      if (splits > 1) us += 3.0 + 8.0 * splits * M * N / 5e6;  // 32-bit parts written and read
+      if (us < best) {
+        best = us;
+        s.tile = i;
+        s.per = per;
+        s.splits = splits;
+      }
+    }
+  }
   return s;
 }
 
@@ -235,15 +288,11 @@ struct Lines {
   bool pad;
   size_t bytes() const { return pad ? up256(2 * (size_t)(rows * pad32(n))) : 0; }
 };
-Lines lines_a(const Product& p) { return {p.at ? p.K : p.M, p.at ? p.M : p.K, p.lda % 8 != 0}; }
-Lines lines_b(const Product& p) { return {p.bt ? p.K : p.N, p.bt ? p.N : p.K, p.ldb % 8 != 0}; }
-
-// Split contractions meet in the join, and results whose rows are not whole 16-byte pieces are written
-// by it.
-bool uses_partial(const Product& p, const Shape& s) { return s.splits > 1 || (!s.stream && !p.out.vec); }
+Lines lines_a(const Product& p) { return {p.at ? p.K : p.M, p.at ? p.M : p.K, p.lda % 8 != 0 && !streams(p)}; }
+Lines lines_b(const Product& p) { return {p.bt ? p.K : p.N, p.bt ? p.N : p.K, p.ldb % 8 != 0 && !streams(p)}; }
 
 size_t partial_bytes(const Product& p, const Shape& s) {
-  if (!uses_partial(p, s)) return 0;
+  if (s.splits == 1) return 0;
   return sizeof(float) * (size_t)s.splits * (p.kind == kProductGated ? 2 : 1) * (size_t)p.N * ((p.M + 7) / 8 * 8);
 }
 
@@ -263,13 +312,22 @@ void launch_tiles(TileArgs& t, const Shape& s, hipStream_t stream) {
   if (KIND == kProductGated) {
     t.k.half_a = (const char*)t.a1 - (const char*)t.a0;
   } else {
-    t.k.half_a = t.k.half_left = (s.tile == 256 ? 128 : 64) * (AT ? 1 : (int64_t)t.k.lda);  // 8 AF rows
+    t.k.half_a = t.k.half_left = (kTiles[s.tile].m / 2) * (AT ? 1 : (int64_t)t.k.lda);  // 8 AF rows
   }
-  const int items = t.m_tiles * t.n_tiles * s.splits, grid = std::min(items, s.tile == 256 ? kCus : 2 * kCus);
-  if (s.tile == 256)
-    tile_product_kernel<8, 4, AT, BT, KIND><<<grid, 512, 0, stream>>>(t);
-  else
-    tile_product_kernel<4, 2, AT, BT, KIND><<<grid, 512, 0, stream>>>(t);
+  const int items = t.m_tiles * t.n_tiles * s.splits, grid = std::min(items, kTiles[s.tile].per_cu * kCus);
+  auto launch = [&](auto ends) {
+    constexpr bool kEnds = decltype(ends)::value;
+    if (s.tile == 0)
+      tile_product_kernel<8, 4, AT, BT, KIND, kEnds><<<grid, 512, 0, stream>>>(t);
+    else if (s.tile == 1)
+      tile_product_kernel<4, 2, AT, BT, KIND, kEnds><<<grid, 512, 0, stream>>>(t);
+    else
+      tile_product_kernel<4, 1, AT, BT, KIND, kEnds><<<grid, 512, 0, stream>>>(t);
+  };
+  if constexpr (KIND == kProductLinear) {
+    if (t.M % 8 == 0) return launch(std::false_type());
+  }
+  launch(std::true_type());
 }
 
 }  // namespace
@@ -307,14 +365,14 @@ dtp_status launch_product_bf16(const Product& p, char* workspace, hipStream_t s)
   t.Mp = (p.M + 7) / 8 * 8;
   t.nq = shape.nq;
   t.per = shape.per;
-  t.partial = uses_partial(p, shape) ? (float*)workspace : nullptr;
+  t.partial = shape.splits > 1 ? (float*)workspace : nullptr;
   t.out = p.out;
   if (shape.stream) {
     StreamArgs r{t.a0, t.a1, t.b, t.k.lda, t.k.ldb, t.M, t.N, t.Mp, p.K, shape.nq, shape.per, shape.splits, t.partial, t.out};
     launch_stream<uint16_t>(p.kind, r, s);
   } else {
-    t.m_tiles = (int)(((int64_t)(p.kind == kProductGated ? 2 : 1) * p.M + shape.tile - 1) / shape.tile);
-    t.n_tiles = (int)((p.N + shape.tile - 1) / shape.tile);
+    t.m_tiles = (int)(((int64_t)(p.kind == kProductGated ? 2 : 1) * p.M + kTiles[shape.tile].m - 1) / kTiles[shape.tile].m);
+    t.n_tiles = (int)((p.N + kTiles[shape.tile].n - 1) / kTiles[shape.tile].n);
     switch (p.kind) {
       case kProductLinear: launch_tiles<kProductLinear, false, false>(t, shape, s); break;
       case kProductGated: launch_tiles<kProductGated, false, false>(t, shape, s); break;

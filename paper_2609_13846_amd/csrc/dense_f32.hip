@@ -29,7 +29,6 @@ struct TileArgs {
   int M, Mp, segments;
   int64_t N;
   int m_tiles, per, stages;  // stages per split, and of a segment
-  bool vec_a, vec_b;         // rows are whole 16-byte pieces
   float* partial;
   ProductOut out;
 };
@@ -42,7 +41,7 @@ struct Stage {
   static constexpr int kFloats = ACROSS ? kStage * kAcrossRow : ROWS * kAlongRow;
   f32x4 v[kPieces];
 
-  __device__ __forceinline__ void load(const float* p, int64_t ld, bool vec, int64_t row0, int64_t rows, int64_t k0,
+  __device__ __forceinline__ void load(const float* p, int64_t ld, int64_t row0, int64_t rows, int64_t k0,
                                        int64_t K) {
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
@@ -52,8 +51,8 @@ struct Stage {
       const bool line = ACROSS ? k < K : row < rows;
       const float* q = p + (ACROSS ? k * ld + row : row * ld + k);
       v[i] = f32x4{};
-      if (line && along + 3 < end && vec) {
-        v[i] = *reinterpret_cast<const f32x4*>(q);
+      if (line && along + 3 < end) {
+        v[i] = *reinterpret_cast<const f32x4_any*>(q);
       } else if (line) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -102,8 +101,8 @@ __global__ void __launch_bounds__(256, 2) tile_product_f32_kernel(TileArgs p) {
     const int64_t k0 = (int64_t)(q - seg * p.stages) * kStage;
 #pragma unroll
     for (int i = 0; i < kMats; ++i)
-      sa[i].load((kGated ? i : seg) ? p.a1 : p.a0, p.lda, p.vec_a, m0, p.M, k0, p.K);
-    sb.load(p.b + (BT ? 0 : seg * p.b_seg), p.ldb, p.vec_b, n0, p.N, k0, p.K);
+      sa[i].load((kGated ? i : seg) ? p.a1 : p.a0, p.lda, m0, p.M, k0, p.K);
+    sb.load(p.b + (BT ? 0 : seg * p.b_seg), p.ldb, n0, p.N, k0, p.K);
   };
   auto store = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
@@ -186,7 +185,7 @@ struct Shape {
 Shape choose(const Product& p) {
   Shape s;
   const bool gated = p.kind == kProductGated;
-  if (!p.at && !p.bt && p.N <= 32 && p.lda % 4 == 0 && p.ldb % 4 == 0) {
+  if (!p.at && !p.bt && p.N <= kStreamTokens) {
     s.stream = true;
     choose_stream<float>(p, s.stages, s.per);
     s.splits = (s.stages + s.per - 1) / s.per;
@@ -253,8 +252,6 @@ dtp_status launch_product_f32(const Product& p, char* workspace, hipStream_t s) 
     t.m_tiles = shape.m_tiles;
     t.per = shape.per;
     t.stages = shape.stages;
-    t.vec_a = p.lda % 4 == 0;
-    t.vec_b = p.ldb % 4 == 0 && p.b_seg % 4 == 0;
     t.partial = partial;
     t.out = p.out;
     switch (p.kind) {

@@ -7,7 +7,7 @@
 
 namespace dtp {
 
-constexpr int kStreamTokens = 64;
+constexpr int kStreamTokens = 16;
 
 struct StreamArgs {
   const void *a0, *a1, *b;
@@ -37,6 +37,16 @@ struct Piece;
 template <>
 struct Piece<uint16_t> {
   typedef bf16x8 V;
+  __device__ static __forceinline__ V load(const uint16_t* p) {
+    return __builtin_bit_cast(V, (u32x4)*reinterpret_cast<const u32x4_any*>(p));
+  }
+  __device__ static __forceinline__ V load_some(const uint16_t* p, int n) {
+    u32x4 v = {};
+#pragma unroll
+    for (int e = 0; e < 7; ++e)
+      if (e < n) v[e / 2] |= (uint32_t)p[e] << (16 * (e % 2));
+    return __builtin_bit_cast(V, v);
+  }
   __device__ static __forceinline__ f32x4 multiply(const V& a, const V& b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
   }
@@ -44,6 +54,14 @@ struct Piece<uint16_t> {
 template <>
 struct Piece<float> {
   typedef f32x4 V;
+  __device__ static __forceinline__ V load(const float* p) { return *reinterpret_cast<const f32x4_any*>(p); }
+  __device__ static __forceinline__ V load_some(const float* p, int n) {
+    V v = {};
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (e < n) v[e] = p[e];
+    return v;
+  }
   __device__ static __forceinline__ f32x4 multiply(const V& a, const V& b, f32x4 c) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
@@ -51,118 +69,109 @@ struct Piece<float> {
   }
 };
 
-// At most 16 TF tokens: the time is that of reading the weights once.  A block takes 16 RF features
-// (gated: of each projection), its eight wavefronts deal out the columns in runs of 128 bytes a
+// At most 16 tokens: the time is that of reading the weights once.  A block takes 16 features (gated:
+// of each projection), its eight wavefronts deal out the columns in runs of 128 bytes a
 // row, and their sums meet in LDS.  Weights and tokens go straight into the matrix instruction's
 // registers: lane l reads 32 bytes of row l % 16, from byte 32 (l / 16) of the run on.  The loads
 // of the next group of runs are in flight while this one's are multiplied.
-template <typename S, int RF, int TF, ProductKind KIND>
+template <typename S, ProductKind KIND>
 __global__ void __launch_bounds__(512, 4) stream_product_kernel(StreamArgs p) {
   using P = Piece<S>;
   using V = typename P::V;
   constexpr bool kGated = KIND == kProductGated;
-  constexpr int kMats = kGated ? 2 : 1, kFrags = kMats * RF;
+  constexpr int kMats = kGated ? 2 : 1;
   constexpr int kWide = 16 / sizeof(S), kRun = 8 * kWide;  // columns of a piece, and of a run
-  constexpr int kGroup = kFrags + TF > 3 ? 1 : 2;          // runs in flight beside those multiplied
-  __shared__ f32x4 sums[8][kFrags * TF][64];
+  constexpr int kGroup = 2;                                // runs in flight beside those multiplied
+  __shared__ f32x4 sums[8][kMats][64];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int r = lane % 16, g = lane / 16;
-  const int m0 = blockIdx.x * 16 * RF;
-  const S *a[kFrags], *b[TF];
+  const int m0 = blockIdx.x * 16, m = min(m0 + r, p.M - 1);
+  const S* a[kMats];
 #pragma unroll
-  for (int i = 0; i < kFrags; ++i) {
-    const int m = min(m0 + 16 * (i % RF) + r, p.M - 1);
-    a[i] = (const S*)(i / RF ? p.a1 : p.a0) + (int64_t)m * p.lda + 2 * kWide * g;
-  }
-#pragma unroll
-  for (int t = 0; t < TF; ++t) b[t] = (const S*)p.b + (int64_t)min(16 * t + r, p.N - 1) * p.ldb + 2 * kWide * g;
-  f32x4 acc[kFrags][TF] = {};
+  for (int i = 0; i < kMats; ++i) a[i] = (const S*)(i ? p.a1 : p.a0) + (int64_t)m * p.lda + 2 * kWide * g;
+  const S* b = (const S*)p.b + (int64_t)min(r, p.N - 1) * p.ldb + 2 * kWide * g;
+  f32x4 acc[kMats] = {};
   const int c0 = blockIdx.y * p.per, c1 = min(c0 + p.per, p.runs);
   const int whole = min(c1, (int)(p.K / kRun));
-  V fa[2][kGroup][kFrags][2], fb[2][kGroup][TF][2];
-  auto fetch = [&](V (&xa)[kGroup][kFrags][2], V (&xb)[kGroup][TF][2], int c) __attribute__((always_inline)) {
+  struct Group {
+    V a[kGroup][kMats][2], b[kGroup][2];
+  };
+  Group x, y;
+  auto fetch = [&](Group& f, int c) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < kGroup; ++u)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int64_t k = (int64_t)(c + 8 * u) * kRun + kWide * h;
 #pragma unroll
-        for (int i = 0; i < kFrags; ++i) xa[u][i][h] = *reinterpret_cast<const V*>(a[i] + k);
-#pragma unroll
-        for (int t = 0; t < TF; ++t) xb[u][t][h] = *reinterpret_cast<const V*>(b[t] + k);
+        for (int i = 0; i < kMats; ++i) f.a[u][i][h] = P::load(a[i] + k);
+        f.b[u][h] = P::load(b + k);
       }
   };
-  auto multiply = [&](const V (&xa)[kGroup][kFrags][2], const V (&xb)[kGroup][TF][2]) __attribute__((always_inline)) {
+  auto multiply = [&](const Group& f) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < kGroup; ++u)
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int i = 0; i < kFrags; ++i)
-#pragma unroll
-          for (int t = 0; t < TF; ++t) acc[i][t] = P::multiply(xa[u][i][h], xb[u][t][h], acc[i][t]);
+        for (int i = 0; i < kMats; ++i) acc[i] = P::multiply(f.a[u][i][h], f.b[u][h], acc[i]);
   };
-  constexpr int kStep = 8 * kGroup;  // runs a group of all wavefronts covers
+  constexpr int kStep = 8 * kGroup;  // runs that a group of all wavefronts covers
   int c = c0 + wave;
-  // groups of this wavefront that are whole: runs c + 8 u < whole
-  const int groups = max(0, (whole - c + 7) / 8 / kGroup);
-  if (groups > 0) fetch(fa[0], fb[0], c);
+  const int groups = max(0, (whole - c + 7) / 8 / kGroup);  // whole ones of this wavefront
+  if (groups > 0) fetch(x, c);
   for (int q = 0; q < groups; q += 2) {
-    if (q + 1 < groups) fetch(fa[1], fb[1], c + kStep);
+    if (q + 1 < groups) fetch(y, c + kStep);
     __builtin_amdgcn_sched_barrier(0);
-    multiply(fa[0], fb[0]);
+    multiply(x);
     if (q + 1 >= groups) break;
-    if (q + 2 < groups) fetch(fa[0], fb[0], c + 2 * kStep);
+    if (q + 2 < groups) fetch(x, c + 2 * kStep);
     __builtin_amdgcn_sched_barrier(0);
-    multiply(fa[1], fb[1]);
+    multiply(y);
     c += 2 * kStep;
   }
-  c = c0 + wave + groups * kStep;
-  for (; c < c1; c += 8)  // single runs, and the one that the columns end in
+  for (c = c0 + wave + groups * kStep; c < c1; c += 8)  // single runs, and the one that the columns end in
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int64_t k = (int64_t)c * kRun + kWide * h;
-      const bool in = k + 2 * kWide * g < p.K;
-      V xa[kFrags] = {};
+      V xb = {}, xa[kMats] = {};
+      const int64_t left = p.K - k - 2 * kWide * g;
+      if (left >= kWide) {
+        xb = P::load(b + k);
 #pragma unroll
-      for (int i = 0; i < kFrags; ++i)
-        if (in) xa[i] = *reinterpret_cast<const V*>(a[i] + k);
+        for (int i = 0; i < kMats; ++i) xa[i] = P::load(a[i] + k);
+      } else if (left > 0) {
+        xb = P::load_some(b + k, (int)left);
 #pragma unroll
-      for (int t = 0; t < TF; ++t) {
-        V xb = {};
-        if (in) xb = *reinterpret_cast<const V*>(b[t] + k);
-#pragma unroll
-        for (int i = 0; i < kFrags; ++i) acc[i][t] = P::multiply(xa[i], xb, acc[i][t]);
+        for (int i = 0; i < kMats; ++i) xa[i] = P::load_some(a[i] + k, (int)left);
       }
+#pragma unroll
+      for (int i = 0; i < kMats; ++i) acc[i] = P::multiply(xa[i], xb, acc[i]);
     }
 #pragma unroll
-  for (int i = 0; i < kFrags; ++i)
-#pragma unroll
-    for (int t = 0; t < TF; ++t) sums[wave][i * TF + t][lane] = acc[i][t];
+  for (int i = 0; i < kMats; ++i) sums[wave][i][lane] = acc[i];
   __syncthreads();
   // a thread per W features of a token; lane 16 (m / 4) + n of a fragment holds rows m .. m + 3
-  constexpr int W = Elem<S>::kWide, kPieces = 16 * RF / W;
-  for (int idx = threadIdx.x; idx < 16 * TF * kPieces; idx += 512) {
-    const int n = idx / kPieces, row = idx % kPieces * W, mm = m0 + row;
-    if (n >= p.N || mm >= p.M) continue;
-    float v[2][W] = {};
+  constexpr int W = Elem<S>::kWide, kPieces = 16 / W;
+  const int n = threadIdx.x / kPieces, row = threadIdx.x % kPieces * W, mm = m0 + row;
+  if (n >= p.N || mm >= p.M) return;
+  float v[2][W] = {};
 #pragma unroll
-    for (int i = 0; i < kMats; ++i)
+  for (int i = 0; i < kMats; ++i)
 #pragma unroll
-      for (int w = 0; w < 8; ++w)
+    for (int w = 0; w < 8; ++w)
 #pragma unroll
-        for (int e = 0; e < W; e += 4) {
-          const f32x4 x = sums[w][(i * RF + row / 16) * TF + n / 16][(row % 16 + e) / 4 * 16 + n % 16];
+      for (int e = 0; e < W; e += 4) {
+        const f32x4 s = sums[w][i][(row + e) / 4 * 16 + n];
 #pragma unroll
-          for (int z = 0; z < 4; ++z) v[i][e + z] += x[z];
-        }
-    if (p.partial) {
-      float* at = p.partial + ((int64_t)blockIdx.y * kMats * p.N + n) * p.Mp + mm;
-      store_partial(at, v[0]);
-      if (kGated) store_partial(at + (int64_t)p.N * p.Mp, v[1]);
-    } else {
-      write_product<S, KIND, W>(p.out, n, mm, p.M, v[0], v[1]);
-    }
+        for (int z = 0; z < 4; ++z) v[i][e + z] += s[z];
+      }
+  if (p.partial) {
+    float* at = p.partial + ((int64_t)blockIdx.y * kMats * p.N + n) * p.Mp + mm;
+    store_partial(at, v[0]);
+    if (kGated) store_partial(at + (int64_t)p.N * p.Mp, v[1]);
+  } else {
+    write_product<S, KIND, W>(p.out, n, mm, p.M, v[0], v[1]);
   }
 }
 
@@ -204,15 +213,7 @@ void choose_stream(const Product& p, int& runs, int& per) {
 
 template <typename S, ProductKind KIND>
 void launch_stream_kind(const StreamArgs& a, hipStream_t s) {
-  // Tokens' pieces are read once per block: two feature fragments share them where there are many.
-  const dim3 one((a.M + 15) / 16, a.splits), two((a.M + 31) / 32, a.splits);
-  if (a.N <= 16)
-    stream_product_kernel<S, 1, 1, KIND><<<one, 512, 0, s>>>(a);
-  else if (a.N <= 32)
-    stream_product_kernel<S, 1, 2, KIND><<<one, 512, 0, s>>>(a);
-  else
-    stream_product_kernel<S, 1, 4, KIND><<<one, 512, 0, s>>>(a);
-  (void)two;
+  stream_product_kernel<S, KIND><<<dim3((a.M + 15) / 16, a.splits), 512, 0, s>>>(a);
 }
 
 template <typename S>

@@ -89,6 +89,7 @@ struct RowPipe {
   static constexpr int kARows = 32 * AF, kHalf = kARows / 2, kBRows = 64 * BF;
   static constexpr int kASlot = kHalf * kRowStage, kBSlot = kBRows * kRowStage;  // bf16 per slot
   static constexpr int kACopies = kHalf / 64, kBCopies = kBRows / 64;  // per wavefront: a half's, and B's
+  static constexpr int kBFirst = (kBCopies + 1) / 2;  // of B's, in step 3; the rest in step 4
   static constexpr int kCopies = 2 * kACopies + kBCopies;
   static constexpr int kH = AF / 2;
   static constexpr int kReadsA = AT ? 2 : 1, kReadsB = BT ? 2 : 1;  // LDS reads per fragment
@@ -191,7 +192,7 @@ struct RowPipe {
   __device__ __forceinline__ void copy_b(uint16_t* slot, const Feed& f, int half) const {
     const __amdgpu_buffer_rsrc_t rsrc = stage_rsrc(f.at.b, f.at.left_b);
 #pragma unroll
-    for (int j = half * (kBCopies / 2); j < (half + 1) * (kBCopies / 2); ++j) {
+    for (int j = half * kBFirst; j < (half ? kBCopies : kBFirst); ++j) {
       const bool out = !BT && (piece_b ^ (32 * (j % 2))) >= f.at.columns;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
           rsrc, (__attribute__((address_space(3))) void*)(slot + (kBCopies * wave + j) * 512), 16,
@@ -322,13 +323,13 @@ struct RowPipe {
       copy_b(cur.b, f, 0);
       read_a(cur.a1, 1, ay);
       multiply(1, ax, b0);
-      order<kH * kReadsA, kBCopies / 2>();
-      meet<kCopies - kBCopies / 2>(settled);  // Y
+      order<kH * kReadsA, kBFirst>();
+      meet<kCopies - (kBCopies - kBFirst)>(settled);  // Y
       copy_b(cur.b, f, 1);
       read_a(next.a0, 0, ax);
       read_b(next.b, 0, b0);
       multiply(1, ay, b1);
-      order<kH * kReadsA + BF * kReadsB, kBCopies / 2>();
+      order<kH * kReadsA + BF * kReadsB, kBCopies - kBFirst>();
     };
     copy_a(s0.a0, f, 0);
     copy_b(s0.b, f, 0);

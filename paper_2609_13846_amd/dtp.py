@@ -140,6 +140,18 @@ def _ptr(x):
     raise TypeError(f"cannot pass {type(x)!r} as a pointer")
 
 
+_DTYPE_NAMES = {}   # torch dtype -> its name
+_TENSOR = None      # torch.Tensor, once a device argument has come
+
+
+def _tensor_type():
+    global _TENSOR
+    if _TENSOR is None:
+        import torch
+        _TENSOR = torch.Tensor
+    return _TENSOR
+
+
 def _dev(t, name, dtypes, numel, optional=False):
     """Address of a device argument after checking it: a contiguous torch tensor on the
     GPU, of one of ``dtypes`` (torch dtype names), with at least ``numel`` elements.  A
@@ -151,12 +163,14 @@ def _dev(t, name, dtypes, numel, optional=False):
         raise ValueError(f"{name} is required")
     if isinstance(t, int):
         return t
-    import torch
-    if not isinstance(t, torch.Tensor):
+    if not isinstance(t, _tensor_type()):
         raise TypeError(f"{name} must be a torch tensor on the GPU, not {type(t).__name__}")
     if not t.is_cuda:
         raise ValueError(f"{name} must be on the GPU (got a tensor on {t.device})")
-    if str(t.dtype).replace("torch.", "") not in dtypes:
+    dtype = t.dtype
+    if dtype not in _DTYPE_NAMES:
+        _DTYPE_NAMES[dtype] = str(dtype).replace("torch.", "")
+    if _DTYPE_NAMES[dtype] not in dtypes:
         raise TypeError(f"{name} must have dtype {' or '.join(dtypes)}, not {t.dtype}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
@@ -181,8 +195,8 @@ def _stream(stream):
     if stream is not None:
         return stream if isinstance(stream, int) else stream.cuda_stream
     import torch
-    if torch.cuda.is_available() and torch.cuda.is_initialized():
-        return torch.cuda.current_stream().cuda_stream
+    if torch.cuda.is_initialized():  # and so a GPU is available, a query that costs more than the rest
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return None
 
 
