@@ -61,7 +61,10 @@ Workspace::~Workspace() {
   if (owned) (void)stream_free(owned, s);
 }
 
-size_t product_bytes(const Product& p) { return p.dtype == DTP_BF16 ? product_bytes_bf16(p) : product_bytes_f32(p); }
+size_t product_bytes(const Product& p) {
+  if (p.N == 0 || p.K == 0) return 0;  // no tokens: nothing is launched
+  return p.dtype == DTP_BF16 ? product_bytes_bf16(p) : product_bytes_f32(p);
+}
 
 dtp_status launch_product(const Product& p, char* workspace, hipStream_t s) {
   return p.dtype == DTP_BF16 ? launch_product_bf16(p, workspace, s) : launch_product_f32(p, workspace, s);

@@ -5,10 +5,9 @@
 // is the operand of four instructions; one that lies across it stays [k][row], a dword per
 // instruction.  Lane l feeds row l % 32 and, in step j of eight columns, column 4 (l / 32) + j, of
 // both operands alike.  The matrix cores need 64 cycles per instruction and 2 to 8 LDS reads
-// per eight instructions, so that loads through registers, one stage ahead, keep up.
-//
-// Sums of 256 columns are added to a total: the rounding of a long contraction grows with the length
-// of its runs, not with its own.
+// per eight instructions, so that loads through registers, one stage ahead, keep up: 8,192 x 4,096
+// x 4,096 in 2.08 to 2.12 ms, 130 TFLOP/s, in either order (a library product 1.82); 2,048 x 1,536 x
+// 512 in 41 us, 256 blocks of 48 stages (29).
 #include <algorithm>
 
 #include "dense_stream.h"
@@ -17,9 +16,8 @@ namespace dtp {
 namespace {
 
 constexpr int kCus = 256;
-constexpr int kStage = 16;                // columns per stage
-constexpr int kAlongRow = kStage + 4;     // floats: 16 rows' 16-byte reads cover the banks once
-constexpr int kFlush = 256 / kStage;      // stages between additions to the totals
+constexpr int kStage = 32;             // columns per stage
+constexpr int kAlongRow = kStage + 4;  // floats: 16 rows' 16-byte reads cover the banks once
 
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 
@@ -33,20 +31,35 @@ struct TileArgs {
   ProductOut out;
 };
 
-// One operand's stage on its way from memory to LDS: ROWS x 16 elements by 256 threads.
-template <int ROWS, bool ACROSS>
+// One operand's stage on its way from memory to LDS: ROWS x kStage elements by THREADS threads.
+template <int ROWS, bool ACROSS, int THREADS>
 struct Stage {
-  static constexpr int kPieces = ROWS * kStage / 4 / 256;
+  static constexpr int kPieces = ROWS * kStage / 4 / THREADS;
   static constexpr int kAcrossRow = ROWS + 8;  // floats: lines 4 apart lie in the other half of the banks
   static constexpr int kFloats = ACROSS ? kStage * kAcrossRow : ROWS * kAlongRow;
+  static constexpr int kAlong = kStage / 4;  // pieces of a row
   f32x4 v[kPieces];
 
-  __device__ __forceinline__ void load(const float* p, int64_t ld, int64_t row0, int64_t rows, int64_t k0,
-                                       int64_t K) {
+  // Rows row0 .. of an operand of `rows` x K, columns k0 .. of the stage.  Whole stages take their
+  // addresses as a uniform base and a lane's offset (`lane_at`, fixed for the launch): formed anew per
+  // piece, with its bounds, they took the vector unit longer than the products the matrix cores.
+  __device__ __forceinline__ static uint32_t lane_at(int64_t ld) {
+    const uint32_t at = threadIdx.x;
+    return ACROSS ? at / (ROWS / 4) * (uint32_t)ld + at % (ROWS / 4) * 4 : at / kAlong * (uint32_t)ld + at % kAlong * 4;
+  }
+  __device__ __forceinline__ void load(const float* p, int64_t ld, int64_t row0, int64_t rows, int64_t k0, int64_t K,
+                                       uint32_t lane) {
+    if (row0 + ROWS <= rows && k0 + kStage <= K) {
+      const float* base = p + (ACROSS ? k0 * ld + row0 : row0 * ld + k0);
+      const int64_t next = ACROSS ? THREADS / (ROWS / 4) * ld : THREADS / kAlong * ld;
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) v[i] = *reinterpret_cast<const f32x4_any*>(base + i * next + lane);
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-      const int at = threadIdx.x + 256 * i;
-      const int64_t row = row0 + (ACROSS ? at % (ROWS / 4) * 4 : at / 4), k = k0 + (ACROSS ? at / (ROWS / 4) : at % 4 * 4);
+      const int at = threadIdx.x + THREADS * i;
+      const int64_t row = row0 + (ACROSS ? at % (ROWS / 4) * 4 : at / kAlong), k = k0 + (ACROSS ? at / (ROWS / 4) : at % kAlong * 4);
       const int64_t along = ACROSS ? row : k, end = ACROSS ? rows : K;
       const bool line = ACROSS ? k < K : row < rows;
       const float* q = p + (ACROSS ? k * ld + row : row * ld + k);
@@ -63,8 +76,8 @@ struct Stage {
   __device__ __forceinline__ void store(float* lds) const {
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-      const int at = threadIdx.x + 256 * i;
-      float* q = ACROSS ? lds + at / (ROWS / 4) * kAcrossRow + at % (ROWS / 4) * 4 : lds + at / 4 * kAlongRow + at % 4 * 4;
+      const int at = threadIdx.x + THREADS * i;
+      float* q = ACROSS ? lds + at / (ROWS / 4) * kAcrossRow + at % (ROWS / 4) * 4 : lds + at / kAlong * kAlongRow + at % kAlong * 4;
       *reinterpret_cast<f32x4*>(q) = v[i];
     }
   }
@@ -79,45 +92,50 @@ struct Stage {
   }
 };
 
-// F x F pieces of 32 x 32 per wavefront (gated: of each projection, F / 2 x F).
+// F x F pieces of 32 x 32 per wavefront (gated: of each projection, F / 2 x F).  With F = 1, where a
+// launch has few tiles, eight wavefronts: two sets that share a stage's columns, whose sums meet
+// in LDS, so that a SIMD has one to multiply while the other reads.
 template <int F, bool AT, bool BT, ProductKind KIND>
-__global__ void __launch_bounds__(256, 2) tile_product_f32_kernel(TileArgs p) {
+__global__ void __launch_bounds__(F > 1 ? 256 : 512, 2) tile_product_f32_kernel(TileArgs p) {
+  constexpr int kSets = F > 1 ? 1 : 2, kThreads = 256 * kSets;
   constexpr bool kGated = KIND == kProductGated;
   constexpr int kTile = 64 * F, kMats = kGated ? 2 : 1, kFM = kGated ? (F > 1 ? F / 2 : 1) : F;
   constexpr int kRowsA = 64 * kFM;  // of each matrix
-  using SA = Stage<kRowsA, AT>;
-  using SB = Stage<kTile, BT>;
+  using SA = Stage<kRowsA, AT, kThreads>;
+  using SB = Stage<kTile, BT, kThreads>;
   __shared__ __attribute__((aligned(16))) float lds[2][kMats * SA::kFloats + SB::kFloats];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int wm = wave & 1, wn = wave >> 1;
+  const int wm = wave & 1, wn = wave >> 1 & 1, set = wave >> 2;
   const int tm = blockIdx.x % p.m_tiles;
   const int64_t m0 = (int64_t)tm * kRowsA, n0 = (int64_t)(blockIdx.x / p.m_tiles) * kTile;
   const int q0 = blockIdx.y * p.per, q1 = min(q0 + p.per, p.stages * p.segments);
-  f32x16 acc[kMats][kFM][F] = {}, total[kMats][kFM][F] = {};
-  SA sa[kMats];
-  SB sb;
+  f32x16 acc[kMats][kFM][F] = {};
+  struct {  // the stage on its way
+    SA a[kMats];
+    SB b;
+  } x;
+  const uint32_t lane_a = SA::lane_at(p.lda), lane_b = SB::lane_at(p.ldb);
   auto load = [&](int q) __attribute__((always_inline)) {
     const int seg = q >= p.stages ? 1 : 0;
     const int64_t k0 = (int64_t)(q - seg * p.stages) * kStage;
 #pragma unroll
     for (int i = 0; i < kMats; ++i)
-      sa[i].load((kGated ? i : seg) ? p.a1 : p.a0, p.lda, m0, p.M, k0, p.K);
-    sb.load(p.b + (BT ? 0 : seg * p.b_seg), p.ldb, n0, p.N, k0, p.K);
+      x.a[i].load((kGated ? i : seg) ? p.a1 : p.a0, p.lda, m0, p.M, k0, p.K, lane_a);
+    x.b.load(p.b + (BT ? 0 : seg * p.b_seg), p.ldb, n0, p.N, k0, p.K, lane_b);
   };
   auto store = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < kMats; ++i) sa[i].store(lds[buf] + i * SA::kFloats);
-    sb.store(lds[buf] + kMats * SA::kFloats);
+    for (int i = 0; i < kMats; ++i) x.a[i].store(lds[buf] + i * SA::kFloats);
+    x.b.store(lds[buf] + kMats * SA::kFloats);
   };
   load(q0);
   store(0);
   __syncthreads();
-  int since = 0;
-  for (int q = q0; q < q1; ++q) {
-    const int buf = (q - q0) & 1;
+  auto stage = [&](int q, int buf) __attribute__((always_inline)) {  // from LDS buffer `buf`
     if (q + 1 < q1) load(q + 1);
 #pragma unroll
-    for (int s = 0; s < kStage / 8; ++s) {
+    for (int i8 = 0; i8 < kStage / 8 / kSets; ++i8) {
+      const int s = set * (kStage / 8 / kSets) + i8;
       f32x4 a[kMats][kFM], b[F];
 #pragma unroll
       for (int m = 0; m < kMats; ++m)
@@ -135,20 +153,34 @@ __global__ void __launch_bounds__(256, 2) tile_product_f32_kernel(TileArgs p) {
             for (int j = 0; j < F; ++j)
               acc[m][i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[m][i][e], b[j][e], acc[m][i][j], 0, 0, 0);
     }
-    if (++since == kFlush) {
-      since = 0;
-#pragma unroll
-      for (int m = 0; m < kMats; ++m)
-#pragma unroll
-        for (int i = 0; i < kFM; ++i)
-#pragma unroll
-          for (int j = 0; j < F; ++j) {
-            total[m][i][j] += acc[m][i][j];
-            acc[m][i][j] = f32x16{};
-          }
-    }
     if (q + 1 < q1) store(buf ^ 1);
     __syncthreads();
+  };
+  for (int q = q0; q < q1; q += 2) {
+    stage(q, 0);
+    if (q + 1 < q1) stage(q + 1, 1);
+  }
+  if constexpr (kSets == 2) {
+    static_assert(F == 1 && sizeof(lds) >= kMats * 16 * 256 * sizeof(float), "the second set's sums fit");
+    f32x4* meet = reinterpret_cast<f32x4*>(&lds[0][0]);
+#pragma unroll
+    for (int m = 0; m < kMats; ++m)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        f32x4* at = meet + ((m * 4 + e) * 4 + (wave & 3)) * 64 + lane;
+        if (set == 1)
+          *at = f32x4{acc[m][0][0][4 * e], acc[m][0][0][4 * e + 1], acc[m][0][0][4 * e + 2], acc[m][0][0][4 * e + 3]};
+      }
+    __syncthreads();
+    if (set == 1) return;
+#pragma unroll
+    for (int m = 0; m < kMats; ++m)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const f32x4 x = meet[((m * 4 + e) * 4 + (wave & 3)) * 64 + lane];
+#pragma unroll
+        for (int z = 0; z < 4; ++z) acc[m][0][0][4 * e + z] += x[z];
+      }
   }
 #pragma unroll
   for (int i = 0; i < kFM; ++i)
@@ -164,7 +196,7 @@ __global__ void __launch_bounds__(256, 2) tile_product_f32_kernel(TileArgs p) {
 #pragma unroll
         for (int x = 0; x < kMats; ++x)
 #pragma unroll
-          for (int z = 0; z < 4; ++z) c[x][z] = acc[x][i][j][4 * e + z] + total[x][i][j][4 * e + z];
+          for (int z = 0; z < 4; ++z) c[x][z] = acc[x][i][j][4 * e + z];
         if (p.partial) {
           float* at = p.partial + ((int64_t)blockIdx.y * kMats * p.N + n) * p.Mp + m;
           store_partial(at, c[0]);
@@ -175,6 +207,10 @@ __global__ void __launch_bounds__(256, 2) tile_product_f32_kernel(TileArgs p) {
       }
     }
 }
+
+// us of a CU per stage and 64 x 64 sums in tiles of 128 and of 64, and of an item that has the CU to
+// itself (in tiles of 128, whose four wavefronts leave the SIMDs one each).
+constexpr double kBig = 0.0140 * kStage, kSmall = 0.0160 * kStage, kBigAlone = 0.0190 * kStage, kSmallAlone = 0.0200 * kStage;
 
 struct Shape {
   bool stream = false;
@@ -192,20 +228,30 @@ Shape choose(const Product& p) {
     return s;
   }
   s.stages = (int)((p.K + kStage - 1) / kStage);
-  auto place = [&](int f) {
-    s.f = f;
-    const int rows = gated ? (f > 1 ? 32 * f : 64) : 64 * f;
-    s.m_tiles = (p.M + rows - 1) / rows;
-    s.n_tiles = (p.N + 64 * f - 1) / (64 * f);
-    return s.m_tiles * s.n_tiles;
-  };
-  int64_t tiles = place(2);
-  if (tiles < 2 * kCus) tiles = place(1);
-  const int64_t nq = (int64_t)s.stages * p.segments;
-  const int64_t want = (4 * kCus + tiles - 1) / tiles;
-  const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({tiles >= 2 * kCus ? 1 : want, nq / 8, 32}));
-  s.per = (int)((nq + splits - 1) / splits);
-  s.splits = (int)((nq + s.per - 1) / s.per);
+  const int nq = s.stages * p.segments;
+  const double planes = gated ? 2.0 : 1.0;
+  double best = 1e30;
+  for (int f = 1; f <= 2; ++f) {
+    const int rows = gated ? 64 : 64 * f;
+    const int64_t m_tiles = (p.M + rows - 1) / rows, n_tiles = (p.N + 64 * f - 1) / (64 * f);
+    const double sums = (gated ? 2.0 : f) * f;  // 64 x 64 of them in a tile
+    for (int splits = 1; splits <= std::min(32, std::max(1, nq / 2)); ++splits) {
+      const int per = (nq + splits - 1) / splits;
+      if ((nq + per - 1) / per != splits) continue;
+      const int64_t items = (m_tiles * n_tiles * splits + kCus - 1) / kCus;  // of a CU
+      const double rate = items > 1 ? (f == 2 ? kBig : kSmall) : (f == 2 ? kBigAlone : kSmallAlone);
+      double us = (double)items * (per * sums * rate + 1.0);
+      if (splits > 1) us += 3.0 + 8.0 * splits * planes * p.M * (double)p.N / 5e6;  // parts written and read
+      if (us < best) {
+        best = us;
+        s.f = f;
+        s.m_tiles = (int)m_tiles;
+        s.n_tiles = n_tiles;
+        s.per = per;
+        s.splits = splits;
+      }
+    }
+  }
   return s;
 }
 
@@ -221,7 +267,7 @@ void launch_tiles(const TileArgs& t, const Shape& s, hipStream_t stream) {
   if (s.f == 2)
     tile_product_f32_kernel<2, AT, BT, KIND><<<grid, 256, 0, stream>>>(t);
   else
-    tile_product_f32_kernel<1, AT, BT, KIND><<<grid, 256, 0, stream>>>(t);
+    tile_product_f32_kernel<1, AT, BT, KIND><<<grid, 512, 0, stream>>>(t);
 }
 
 }  // namespace

@@ -152,6 +152,19 @@ def _tensor_type():
     return _TENSOR
 
 
+def _on_gpu(t, name, dtypes):
+    """Refuses what is not a torch tensor on the GPU of one of ``dtypes``."""
+    if not isinstance(t, _tensor_type()):
+        raise TypeError(f"{name} must be a torch tensor on the GPU, not {type(t).__name__}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on the GPU (got a tensor on {t.device})")
+    dtype = t.dtype
+    if dtype not in _DTYPE_NAMES:
+        _DTYPE_NAMES[dtype] = str(dtype).replace("torch.", "")
+    if _DTYPE_NAMES[dtype] not in dtypes:
+        raise TypeError(f"{name} must have dtype {' or '.join(dtypes)}, not {t.dtype}")
+
+
 def _dev(t, name, dtypes, numel, optional=False):
     """Address of a device argument after checking it: a contiguous torch tensor on the
     GPU, of one of ``dtypes`` (torch dtype names), with at least ``numel`` elements.  A
@@ -163,15 +176,7 @@ def _dev(t, name, dtypes, numel, optional=False):
         raise ValueError(f"{name} is required")
     if isinstance(t, int):
         return t
-    if not isinstance(t, _tensor_type()):
-        raise TypeError(f"{name} must be a torch tensor on the GPU, not {type(t).__name__}")
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be on the GPU (got a tensor on {t.device})")
-    dtype = t.dtype
-    if dtype not in _DTYPE_NAMES:
-        _DTYPE_NAMES[dtype] = str(dtype).replace("torch.", "")
-    if _DTYPE_NAMES[dtype] not in dtypes:
-        raise TypeError(f"{name} must have dtype {' or '.join(dtypes)}, not {t.dtype}")
+    _on_gpu(t, name, dtypes)
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     if t.numel() < numel:
@@ -511,17 +516,17 @@ def dtp_gated_backward(n_tokens, d_model, n_neurons, dtype, x, w_gate, w_up, pre
 def _heads(t, name, dtypes, n_tokens, heads, head_dim):
     """(address, elements between tokens) of a [n_tokens, heads, head_dim] GPU tensor whose tokens may
     lie apart, as a slice of a packed projection's rows does."""
-    import torch
-    if not isinstance(t, torch.Tensor) or t.dim() != 3:
+    if not isinstance(t, _tensor_type()) or t.dim() != 3:
         raise TypeError(f"{name} must be a torch tensor of 3 dimensions on the GPU")
-    if tuple(t.shape) != (n_tokens, heads, head_dim):
+    if t.shape != (n_tokens, heads, head_dim):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, the call needs {(n_tokens, heads, head_dim)}")
-    stride = t.stride(0) if n_tokens > 1 else heads * head_dim
-    if n_tokens:
-        if (t.stride(2) != 1 and head_dim > 1) or (t.stride(1) != head_dim and heads > 1):
-            raise ValueError(f"{name}: the heads of a token must be contiguous")
-        _dev(t[0], name, dtypes, 0)
-    return t.data_ptr(), stride
+    if n_tokens == 0:
+        return t.data_ptr(), heads * head_dim
+    token, head, column = t.stride()
+    if (column != 1 and head_dim > 1) or (head != head_dim and heads > 1):
+        raise ValueError(f"{name}: the heads of a token must be contiguous")
+    _on_gpu(t, name, dtypes)
+    return t.data_ptr(), token if n_tokens > 1 else heads * head_dim
 
 
 def _rotation(positions, inv_freq, n_tokens):
@@ -529,8 +534,7 @@ def _rotation(positions, inv_freq, n_tokens):
         raise ValueError("positions and inv_freq must be given together")
     if positions is None:
         return None, None, 0
-    import torch
-    if not isinstance(inv_freq, torch.Tensor):
+    if not isinstance(inv_freq, _tensor_type()):
         raise TypeError("inv_freq must be a torch tensor on the GPU")
     return (_dev(positions, "positions", ("int32",), n_tokens), _dev(inv_freq, "inv_freq", _F, 0),
             2 * inv_freq.numel())
