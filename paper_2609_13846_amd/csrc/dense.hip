@@ -181,20 +181,26 @@ dtp_status fill_zeros(void* p, int64_t n, int dtype, hipStream_t s) {
 
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
-int64_t sum_chunk_rows(int64_t T) { return std::max<int64_t>(64, (T + 511) / 512); }
-int64_t sum_chunks(int64_t T) { return (T + sum_chunk_rows(T) - 1) / sum_chunk_rows(T); }
+// Rows per chunk of a column sum, a multiple of the eight that a block takes at a time: 64, and fewer
+// where that would be under a thousand blocks; at most 512 chunks.
+int64_t sum_chunk_rows(int64_t T, int N) {
+  const int64_t groups = (N + kSumCols - 1) / kSumCols;
+  const int64_t rows = std::max<int64_t>(8, std::min<int64_t>(64, (T * groups / 1024 + 7) / 8 * 8));
+  return std::max<int64_t>(rows, ((T + 511) / 512 + 7) / 8 * 8);
+}
+int64_t sum_chunks(int64_t T, int N) { return (T + sum_chunk_rows(T, N) - 1) / sum_chunk_rows(T, N); }
 
 // dbias = sum over the tokens of scale act'(z) dy.
 dtp_status launch_column_sums(const void* dy, const float* pre, int act, float scale, int64_t T, int N, int dtype,
                               void* out, float* partial, hipStream_t s) {
-  const int chunks = (int)sum_chunks(T);
+  const int chunks = (int)sum_chunks(T, N);
   const dim3 grid((N + kSumCols - 1) / kSumCols, chunks);
   if (dtype == DTP_BF16) {
-    column_sums_kernel<<<grid, 256, 0, s>>>((const uint16_t*)dy, pre, act, scale, T, N, sum_chunk_rows(T), 
+    column_sums_kernel<<<grid, 256, 0, s>>>((const uint16_t*)dy, pre, act, scale, T, N, sum_chunk_rows(T, N), 
                                             partial);
     join_sums_kernel<<<(N + 31) / 32, 256, 0, s>>>(partial, chunks, N, (uint16_t*)out);
   } else {
-    column_sums_kernel<<<grid, 256, 0, s>>>((const float*)dy, pre, act, scale, T, N, sum_chunk_rows(T), 
+    column_sums_kernel<<<grid, 256, 0, s>>>((const float*)dy, pre, act, scale, T, N, sum_chunk_rows(T, N), 
                                             partial);
     join_sums_kernel<<<(N + 31) / 32, 256, 0, s>>>(partial, chunks, N, (float*)out);
   }
@@ -282,7 +288,7 @@ Plan backward_plan(int64_t T, int K, int N, int parts, int dtype, bool pass, boo
   size_t at = 0;
   if (pass) at = up256(esize(dtype) * (size_t)T * parts * w.ld);
   w.sums = at;
-  if (sums) at += up256(sizeof(float) * (size_t)sum_chunks(T) * N);
+  if (sums) at += up256(sizeof(float) * (size_t)sum_chunks(T, N) * N);
   w.scratch = at;
   w.bytes = at + std::max(product_bytes(dx_product(T, K, N, parts, w.ld, dtype)),
                           product_bytes(dw_product(T, K, N, parts, w.ld, dtype)));

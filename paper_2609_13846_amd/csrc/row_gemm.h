@@ -21,16 +21,16 @@
 // columns in two LDS slots.  A wavefront's A fragments come in two halves, and a stage is four
 // steps of AF / 2 x BF products:
 //   1  half 0, columns  0-31   reads half 0, columns 32-63, and B's columns 32-63
-//                              copies half 1 of the next stage
 //   X  barrier: all have read half 0 and B; half 1 has landed
-//   2  half 0, columns 32-63   reads half 1, columns  0-31;  copies half 0, two stages on
-//   3  half 1, columns  0-31   reads half 1, columns 32-63;  copies B, two stages on
+//   2  half 0, columns 32-63   reads half 1, columns  0-31;  copies half 0 and some of B two stages on
+//   3  half 1, columns  0-31   reads half 1, columns 32-63;  copies the rest of B
 //   Y  barrier: all have read half 1; the next stage's half 0 and B have landed
-//   4  half 1, columns 32-63   reads the next stage's first fragments;  copies the rest of B
-// so that every fragment is read a step before its products, a copy has three to five steps to
+//   4  half 1, columns 32-63   reads the next stage's first fragments;  copies half 1 two stages on
+// so that every fragment is read a step before its products, a copy has five to seven steps to
 // land, and the copies, which a wavefront cannot pass while the path to L2 is busy, are shared out
-// evenly.  The stages of a block's items follow each other without a gap: the copies run ahead
-// into the next item while the results of this one are written.
+// (all between X and Y: 2 to 5% slower).  In a step the first product goes before the reads and
+// copies of its column (1 to 2%).  The stages of a block's items follow each other without a gap:
+// the copies run two stages ahead into the next item while the results of this one are written.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -89,7 +89,7 @@ struct RowPipe {
   static constexpr int kARows = 32 * AF, kHalf = kARows / 2, kBRows = 64 * BF;
   static constexpr int kASlot = kHalf * kRowStage, kBSlot = kBRows * kRowStage;  // bf16 per slot
   static constexpr int kACopies = kHalf / 64, kBCopies = kBRows / 64;  // per wavefront: a half's, and B's
-  static constexpr int kBFirst = (kBCopies + 1) / 2;  // of B's, in step 3; the rest in step 4
+  static constexpr int kBFirst = kBCopies > 2 ? 1 : 0;  // of B's, in step 2; the rest in step 3
   static constexpr int kCopies = 2 * kACopies + kBCopies;
   static constexpr int kH = AF / 2;
   static constexpr int kReadsA = AT ? 2 : 1, kReadsB = BT ? 2 : 1;  // LDS reads per fragment
@@ -188,11 +188,12 @@ struct RowPipe {
           (int)(out ? kOutOfRange : va[j]), 0, 0, 0);
     }
   }
-  // Half `half` of the wavefront's copies of B.
-  __device__ __forceinline__ void copy_b(uint16_t* slot, const Feed& f, int half) const {
+  // The wavefront's copies FROM .. TO - 1 of B.
+  template <int FROM, int TO>
+  __device__ __forceinline__ void copy_b(uint16_t* slot, const Feed& f) const {
     const __amdgpu_buffer_rsrc_t rsrc = stage_rsrc(f.at.b, f.at.left_b);
 #pragma unroll
-    for (int j = half * kBFirst; j < (half ? kBCopies : kBFirst); ++j) {
+    for (int j = FROM; j < TO; ++j) {
       const bool out = !BT && (piece_b ^ (32 * (j % 2))) >= f.at.columns;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
           rsrc, (__attribute__((address_space(3))) void*)(slot + (kBCopies * wave + j) * 512), 16,
@@ -200,16 +201,15 @@ struct RowPipe {
     }
   }
 
-  // Waits until this wavefront's LDS reads are done and its copies but the last N have landed
+  // Waits until this wavefront's LDS reads are done and its copies but a stage's, the last, have landed
   // (unless they are known to have), then for the block.
-  template <int N>
   __device__ __forceinline__ void meet(int& settled) const {
     asm volatile("" ::: "memory");  // no LDS access moves across the barrier
     if (settled > 0) {
       --settled;
       __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
     } else {
-      __builtin_amdgcn_s_waitcnt(0x0070 | N);  // vmcnt(N), lgkmcnt(0)
+      __builtin_amdgcn_s_waitcnt(0x0070 | kCopies);  // vmcnt(kCopies), lgkmcnt(0)
     }
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
@@ -309,37 +309,37 @@ struct RowPipe {
     };
     int pairs = f.at.n / 2, settled = 0;
     auto stage = [&](Slot cur, Slot next) __attribute__((always_inline)) {
-      copy_a(next.a1, f, 1);
       read_a(cur.a0, 1, ay);
       read_b(cur.b, 1, b1);
       multiply(0, ax, b0);
-      order<kH * kReadsA + BF * kReadsB, kACopies>();
-      meet<kCopies>(settled);  // X
-      advance();
+      order<kH * kReadsA + BF * kReadsB, 0>();
+      meet(settled);  // X
       copy_a(cur.a0, f, 0);
+      copy_b<0, kBFirst>(cur.b, f);
       read_a(cur.a1, 0, ax);
       multiply(0, ay, b1);
-      order<kH * kReadsA, kACopies>();
-      copy_b(cur.b, f, 0);
+      order<kH * kReadsA, kACopies + kBFirst>();
+      copy_b<kBFirst, kBCopies>(cur.b, f);
       read_a(cur.a1, 1, ay);
       multiply(1, ax, b0);
-      order<kH * kReadsA, kBFirst>();
-      meet<kCopies - (kBCopies - kBFirst)>(settled);  // Y
-      copy_b(cur.b, f, 1);
+      order<kH * kReadsA, kBCopies - kBFirst>();
+      meet(settled);  // Y
+      copy_a(cur.a1, f, 1);
       read_a(next.a0, 0, ax);
       read_b(next.b, 0, b0);
       multiply(1, ay, b1);
-      order<kH * kReadsA + BF * kReadsB, kBCopies - kBFirst>();
+      order<kH * kReadsA + BF * kReadsB, kACopies>();
+      advance();
     };
-    copy_a(s0.a0, f, 0);
-    copy_b(s0.b, f, 0);
-    copy_b(s0.b, f, 1);
-    copy_a(s0.a1, f, 1);
-    advance();
-    copy_a(s1.a0, f, 0);
-    copy_b(s1.b, f, 0);
-    copy_b(s1.b, f, 1);
-    meet<kCopies>(settled);
+    auto whole = [&](Slot s) __attribute__((always_inline)) {
+      copy_a(s.a0, f, 0);
+      copy_b<0, kBCopies>(s.b, f);
+      copy_a(s.a1, f, 1);
+      advance();
+    };
+    whole(s0);
+    whole(s1);
+    meet(settled);
     read_a(s0.a0, 0, ax);
     read_b(s0.b, 0, b0);
     for (;;) {
@@ -348,7 +348,7 @@ struct RowPipe {
         stage(s0, s1);
         stage(s1, s0);
       }
-      settled = 2;  // done() waits for the copies in flight
+      settled = 3;  // done() waits for the copies in flight
       done(index);
       index += stride;
       if (index >= count) break;
