@@ -210,7 +210,7 @@ __global__ void __launch_bounds__(F > 1 ? 256 : 512, 2) tile_product_f32_kernel(
 
 // us of a CU per stage and 64 x 64 sums in tiles of 128 and of 64, and of an item that has the CU to
 // itself (in tiles of 128, whose four wavefronts leave the SIMDs one each).
-constexpr double kBig = 0.0140 * kStage, kSmall = 0.0160 * kStage, kBigAlone = 0.0190 * kStage, kSmallAlone = 0.0200 * kStage;
+constexpr double kBig = 0.0158 * kStage, kSmall = 0.0195 * kStage, kBigAlone = 0.0190 * kStage, kSmallAlone = 0.0260 * kStage;
 
 struct Shape {
   bool stream = false;
