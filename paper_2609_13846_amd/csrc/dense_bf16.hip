@@ -27,37 +27,33 @@ struct TileArgs {
   ProductOut out;
 };
 
-// Kept pre-activations are read a whole pass later, from memory.
-__device__ __forceinline__ void store_kept(float* p, const float (&v)[8]) {
-#pragma unroll
-  for (int i = 0; i < 8; i += 4)
-    __builtin_nontemporal_store(f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]}, reinterpret_cast<f32x4_any*>(p + i));
-}
-
 __device__ __forceinline__ float half_of(const u32x4& v, int e) {
   return __uint_as_float(e % 2 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16);
 }
-template <bool PAST>
-__device__ __forceinline__ void store_whole(uint16_t* p, const float (&v)[8]) {
+__device__ __forceinline__ u32x4 pack_whole(const float (&v)[8]) {
   u32x4 o;
 #pragma unroll
   for (int e = 0; e < 4; ++e) o[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
-  if constexpr (PAST)
-    __builtin_nontemporal_store(o, reinterpret_cast<u32x4_any*>(p));
-  else
-    *reinterpret_cast<u32x4_any*>(p) = o;
+  return o;
 }
 
-// write_product for eight whole features; PAST: past the caches.
-template <ProductKind KIND, bool PAST>
-__device__ __forceinline__ void write_whole(const ProductOut& o, int64_t n, int m, int M, const float (&c0)[8],
-                                            const float (&c1)[8], const u32x4& bias, const u32x4& residual) {
+// 16 bytes at any address; PAST: past the caches.
+template <bool PAST, typename T>
+__device__ __forceinline__ void put(T* p, const u32x4& v) {
+  if constexpr (PAST)
+    __builtin_nontemporal_store(v, reinterpret_cast<u32x4_any*>(p));
+  else
+    *reinterpret_cast<u32x4_any*>(p) = v;
+}
+
+// The eight results of a place, from their sums; bias and residual are theirs.
+template <ProductKind KIND>
+__device__ __forceinline__ u32x4 finish(const ProductOut& o, const float (&c0)[8], const float (&c1)[8],
+                                        const u32x4& residual) {
   float v[8];
-  uint16_t *const y1 = (uint16_t*)o.y, *const y2 = (uint16_t*)o.y2;
-  if constexpr (KIND == kProductLinear) {
+  if constexpr (KIND == kProductLinear) {  // c0: with the bias
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = c0[e] + half_of(bias, e);
-    if (o.pre) store_kept(o.pre + n * M + m, v);
+    for (int e = 0; e < 8; ++e) v[e] = c0[e];
     if (o.act != DTP_ACT_NONE) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = activate<uint16_t>(o.act, v[e]);
@@ -69,28 +65,42 @@ __device__ __forceinline__ void write_whole(const ProductOut& o, int64_t n, int 
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] *= o.alpha;
     }
-    store_whole<PAST>((uint16_t*)o.y + n * M + m, v);
   } else if constexpr (KIND == kProductGated) {
-    if (o.pre) {
-      store_kept(o.pre + 2 * n * M + m, c0);
-      store_kept(o.pre + (2 * n + 1) * M + m, c1);
-    }
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = activate<uint16_t>(o.act, c0[e]) * c1[e];
-    store_whole<PAST>((uint16_t*)o.y + n * M + m, v);
   } else {
-    const bool second = n >= o.n_split;
-    const int64_t row = second ? n - o.n_split : n;
-    if (row >= o.n_keep) return;
-    uint16_t* const y = second ? y2 : y1;
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = o.alpha * c0[e];
-    store_whole<PAST>(y + row * M + m, v);
+  }
+  return pack_whole(v);
+}
+
+// Lanes r and r + 8 of 16: a keeps its lower eight lanes and takes b's in the upper ones, b the
+// other way round: what was 16 rows of a and of b is 8 rows of a and b, and then the other 8.
+__device__ __forceinline__ void exchange_rows(u32x4& a, u32x4& b) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int x = (int)a[e], y = (int)b[e];
+    a[e] = (uint32_t)__builtin_amdgcn_update_dpp(x, y, 0x128, 0xf, 0xc, false);  // row_ror:8
+    b[e] = (uint32_t)__builtin_amdgcn_update_dpp(y, x, 0x128, 0xf, 0x3, false);
   }
 }
 
-// One block per CU (256 x 256 tiles; two of 128 x 128, three of 128 x 64), each with a run of items: a tile, or a split of
-// its contraction.  Items are numbered so that the ones that run together on an XCD share operands.
+// Eight consecutive values per lane group of 16, as a lane's lower and upper four: afterwards a holds
+// the 16 lower ones of the four groups' 32 and b the upper, four consecutive in each group.
+__device__ __forceinline__ void exchange_groups(u32x4& a, u32x4& b) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const auto half = __builtin_amdgcn_permlane16_swap(a[e], b[e], false, false);
+    const auto whole = __builtin_amdgcn_permlane32_swap(half[0], half[1], false, false);
+    a[e] = whole[0];
+    b[e] = whole[1];
+  }
+}
+
+// One block per CU (256 x 256 tiles; two of 128 x 128, three of 128 x 64), each with a run of items: a tile, or a
+// split of its contraction.  Items are numbered so that the ones that run together on an XCD share
+// operands.
 // ENDS: M need not be a multiple of 8.  (A kernel of its own for the linear epilogue, whose registers
 // the path for rows' ends would spill: 735 -> 829 us for 65,536 x 1,024 x 6,144.)
 template <int AF, int BF, bool AT, bool BT, ProductKind KIND, bool ENDS>
@@ -103,7 +113,7 @@ __global__ void __launch_bounds__(512, AF * BF > 16 ? 2 : 4) tile_product_kernel
   // them, where they would displace the operands: 65,536 x 1,024 x 6,144 729 -> 704 us, a gated block
   // that keeps its pre-activations 950 -> 915.  (Gradients' are not: dx of 16,384 x 4,096 x 1,536
   // took 166 us instead of 161.)
-  constexpr bool kPast = AF * BF > 16 && KIND != kProductGrad;
+  constexpr bool kPast = AF * BF > 16 && KIND != kProductGrad, kLines = kPast && kGated;
   __shared__ __attribute__((aligned(16))) uint16_t s0a0[Pipe::kASlot], s0a1[Pipe::kASlot], s0b[Pipe::kBSlot],
       s1a0[Pipe::kASlot], s1a1[Pipe::kASlot], s1b[Pipe::kBSlot];
   const int tiles = p.m_tiles * p.n_tiles;
@@ -191,17 +201,77 @@ __global__ void __launch_bounds__(512, AF * BF > 16 ? 2 : 4) tile_product_kernel
                                                                (int64_t)(n_lane + 16 * j) * p.M + m_lane + 32 * i);
     };
     fetch(0);
+    // A gated block's results go in whole 128-byte lines, eight rows at a time: the lanes' values change
+    // places first.  (In halves and quarters of lines, past the caches, memory took 15 to 30% more
+    // bytes: 918 us for 65,536 tokens that keep their pre-activations, and 867.  The linear
+    // epilogue's registers would spill: 707 us for 65,536 x 1,024 x 6,144 became 772.)
+    const int r8 = pipe.lane % 8, upper = pipe.lane % 16 / 8, group = pipe.lane / 16;
+    const int m_wave = m_lane - 8 * group, n_wave = n_lane - pipe.lane % 16;
+    auto store_kept = [&](int plane, int i, int j, const float (&c)[8]) __attribute__((always_inline)) {
+      if constexpr (kLines) {
+        u32x4 x, y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[e] = __float_as_uint(c[e]);
+          y[e] = __float_as_uint(c[4 + e]);
+        }
+        exchange_groups(x, y);
+        exchange_rows(x, y);
+        const int m = m_wave + 32 * i + 16 * upper + 4 * group;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int n = n_wave + 16 * j + 8 * h + r8;
+          if (n >= p.N || m >= p.M) continue;
+          float* at = p.out.pre + ((int64_t)n * (kGated ? 2 : 1) + plane) * p.M + m;
+          put<kPast>(at, h ? y : x);
+        }
+      } else {
+        const int n = n_lane + 16 * j, m = m_lane + 32 * i;
+        if (n >= p.N || m >= p.M) return;
+        float* at = p.out.pre + ((int64_t)n * (kGated ? 2 : 1) + plane) * p.M + m;
+        put<kPast>(at, u32x4{__float_as_uint(c[0]), __float_as_uint(c[1]), __float_as_uint(c[2]), __float_as_uint(c[3])});
+        put<kPast>(at + 4, u32x4{__float_as_uint(c[4]), __float_as_uint(c[5]), __float_as_uint(c[6]), __float_as_uint(c[7])});
+      }
+    };
 #pragma unroll
     for (int j = 0; j < BF; ++j) {
       if (j + 1 < BF) fetch(j + 1);
       if (j == 0) pipe.settle();
+      u32x4 out[kPairs];
 #pragma unroll
       for (int i = 0; i < kPairs; ++i) {
         const int n = n_lane + 16 * j, m = m_lane + 32 * i;
-        if (n >= p.N || m >= p.M) continue;
+        if (!kLines && (n >= p.N || m >= p.M)) continue;
         float c0[8], c1[8];
         sums(i, j, c0, c1);
-        write_whole<KIND, kPast>(p.out, n, m, p.M, c0, c1, bias[i], residual[j % 2][i]);
+        if (kLinear) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) c0[e] += half_of(bias[i], e);
+        }
+        if (KIND != kProductGrad && p.out.pre) {
+          store_kept(0, i, j, c0);
+          if (kGated) store_kept(1, i, j, c1);
+        }
+        out[i] = finish<KIND>(p.out, c0, c1, residual[j % 2][i]);
+        if constexpr (!kLines) {
+          uint16_t *const y1 = (uint16_t*)p.out.y, *const y2 = (uint16_t*)p.out.y2;
+          const bool second = KIND == kProductGrad && n >= p.out.n_split;
+          const int64_t row = second ? n - p.out.n_split : n;
+          if (KIND == kProductGrad && row >= p.out.n_keep) continue;
+          put<kPast>((second ? y2 : y1) + row * p.M + m, out[i]);
+        }
+      }
+      if constexpr (kLines) {
+#pragma unroll
+        for (int i = 0; i < kPairs; i += 2) {
+          exchange_rows(out[i], out[i + 1]);
+          const int m = m_wave + 32 * (i + upper) + 8 * group;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int n = n_wave + 16 * j + 8 * h + r8;
+            if (n < p.N && m < p.M) put<kPast>((uint16_t*)p.out.y + (int64_t)n * p.M + m, out[i + h]);
+          }
+        }
       }
     }
   };
