@@ -101,8 +101,8 @@ __device__ __forceinline__ void exchange_groups(u32x4& a, u32x4& b) {
 // One block per CU (256 x 256 tiles; two of 128 x 128, three of 128 x 64), each with a run of items: a tile, or a
 // split of its contraction.  Items are numbered so that the ones that run together on an XCD share
 // operands.
-// ENDS: M need not be a multiple of 8.  (A kernel of its own for the linear epilogue, whose registers
-// the path for rows' ends would spill: 735 -> 829 us for 65,536 x 1,024 x 6,144.)
+// ENDS: M need not be a multiple of 8.  (A kernel of its own for the linear epilogue, which has no
+// registers for the rows' ends beside the exchange of lines.)
 template <int AF, int BF, bool AT, bool BT, ProductKind KIND, bool ENDS>
 __global__ void __launch_bounds__(512, AF * BF > 16 ? 2 : 4) tile_product_kernel(TileArgs p) {
   constexpr bool kGated = KIND == kProductGated;
@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(512, AF * BF > 16 ? 2 : 4) tile_product_kernel
   // them, where they would displace the operands: 65,536 x 1,024 x 6,144 729 -> 704 us, a gated block
   // that keeps its pre-activations 950 -> 915.  (Gradients' are not: dx of 16,384 x 4,096 x 1,536
   // took 166 us instead of 161.)
-  constexpr bool kPast = AF * BF > 16 && KIND != kProductGrad, kLines = kPast && kGated;
+  constexpr bool kPast = AF * BF > 16 && KIND != kProductGrad, kLines = kPast && (kGated || !ENDS);
   __shared__ __attribute__((aligned(16))) uint16_t s0a0[Pipe::kASlot], s0a1[Pipe::kASlot], s0b[Pipe::kBSlot],
       s1a0[Pipe::kASlot], s1a1[Pipe::kASlot], s1b[Pipe::kBSlot];
   const int tiles = p.m_tiles * p.n_tiles;
@@ -201,10 +201,10 @@ __global__ void __launch_bounds__(512, AF * BF > 16 ? 2 : 4) tile_product_kernel
                                                                (int64_t)(n_lane + 16 * j) * p.M + m_lane + 32 * i);
     };
     fetch(0);
-    // A gated block's results go in whole 128-byte lines, eight rows at a time: the lanes' values change
-    // places first.  (In halves and quarters of lines, past the caches, memory took 15 to 30% more
-    // bytes: 918 us for 65,536 tokens that keep their pre-activations, and 867.  The linear
-    // epilogue's registers would spill: 707 us for 65,536 x 1,024 x 6,144 became 772.)
+    // Results past the caches go in whole 128-byte lines, eight rows at a time: the lanes' values
+    // change places first.  (In halves and quarters of lines memory took 15 to 35% more bytes:
+    // 918 us for a gated block over 65,536 tokens that keeps its pre-activations, and 867; 877 for
+    // 65,536 x 1,024 x 6,144 with bias and residual, and 837.)
     const int r8 = pipe.lane % 8, upper = pipe.lane % 16 / 8, group = pipe.lane / 16;
     const int m_wave = m_lane - 8 * group, n_wave = n_lane - pipe.lane % 16;
     auto store_kept = [&](int plane, int i, int j, const float (&c)[8]) __attribute__((always_inline)) {

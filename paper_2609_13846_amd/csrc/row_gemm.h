@@ -353,6 +353,9 @@ struct RowPipe {
       index += stride;
       if (index >= count) break;
       pairs = item(index).n / 2;
+      // once more: kept from the last step on, they would take registers from done()
+      read_a(s0.a0, 0, ax);
+      read_b(s0.b, 0, b0);
     }
     __builtin_amdgcn_s_waitcnt(0x0070);  // nothing lands in LDS after the block is done
     __syncthreads();
