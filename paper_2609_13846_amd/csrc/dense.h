@@ -56,11 +56,11 @@ struct Range {  // a buffer of the caller's
   size_t bytes;
   const char* name;
   int align = 16;
-  const void* may_be = nullptr;  // the one input that an output may be in place of
+  int in_place = -1;  // the one input, by its place in the list, that an output may be in place of
 };
 // Alignment, memory and room of the buffers that are not NULL.
 dtp_status check_ranges(const Range* r, int n);
-// No output overlaps an input (but in place where `may_be` says so) or another output.
+// No output overlaps an input (but in place where `in_place` says so) or another output.
 dtp_status check_disjoint(const Range* outs, int n_outs, const Range* ins, int n_ins);
 
 // A call's scratch: the caller's workspace, or stream-ordered memory that is returned with it.

@@ -16,7 +16,7 @@ dtp_status check_disjoint(const Range* outs, int n_outs, const Range* ins, int n
   };
   for (int i = 0; i < n_outs; ++i) {
     for (int j = 0; j < n_ins; ++j)
-      DTP_CHECK(!overlap(outs[i], ins[j]) || (outs[i].may_be == ins[j].p && outs[i].p == ins[j].p && outs[i].p),
+      DTP_CHECK(!overlap(outs[i], ins[j]) || (outs[i].in_place == j && outs[i].p == ins[j].p),
                 DTP_ERR_INVALID_ARG, "%s overlaps %s", outs[i].name, ins[j].name);
     for (int j = i + 1; j < n_outs; ++j)
       DTP_CHECK(!overlap(outs[i], outs[j]), DTP_ERR_INVALID_ARG, "%s overlaps %s", outs[i].name, outs[j].name);
@@ -326,11 +326,10 @@ dtp_status forward(ProductKind kind, int64_t T, int K, int N, int dtype, const v
   const size_t es = esize(dtype), nx = es * T * K, nw = es * (size_t)N * K, ny = es * T * N;
   const Range in[] = {{x, nx, "x"}, {w.w0, nw, gated ? "w_gate" : "w"}, {w.w1, nw, "w_up"},
                       {bias, es * N, "bias"}, {residual, ny, "residual"}};
-  Range out[] = {{y, ny, gated ? "h" : "y"}, {pre, sizeof(float) * T * N * (gated ? 2 : 1), "pre"},
+  const Range out[] = {{y, ny, gated ? "h" : "y", 16, 4}, {pre, sizeof(float) * T * N * (gated ? 2 : 1), "pre"},
                  {workspace, (size_t)std::max<int64_t>(given_bytes, 0), "workspace"}};
-  out[0].may_be = residual;
-  if ((st = check_ranges(in, 5)) != DTP_OK || (st = check_ranges(out, 2)) != DTP_OK ||
-      (st = check_disjoint(out, 3, in, 5)) != DTP_OK)
+  if ((st = check_disjoint(out, 3, in, 5)) != DTP_OK || (st = check_ranges(in, 5)) != DTP_OK ||
+      (st = check_ranges(out, 2)) != DTP_OK)
     return st;
   Product p = forward_product(kind, T, K, N, dtype);
   p.a0 = w.w0;
@@ -371,8 +370,8 @@ dtp_status backward(ProductKind kind, int64_t T, int K, int N, int dtype, const 
                       {T && with_act ? pre : nullptr, sizeof(float) * T * N * parts, "pre"}};
   const Range out[] = {{T ? dx : nullptr, nx, "dx"}, {dw0, nw, gated ? "dw_gate" : "dw"}, {dw1, nw, "dw_up"},
                        {db, es * N, "dbias"}, {workspace, (size_t)std::max<int64_t>(given_bytes, 0), "workspace"}};
-  if ((st = check_ranges(in, 5)) != DTP_OK || (st = check_ranges(out, 4)) != DTP_OK ||
-      (st = check_disjoint(out, 5, in, 5)) != DTP_OK)
+  if ((st = check_disjoint(out, 5, in, 5)) != DTP_OK || (st = check_ranges(in, 5)) != DTP_OK ||
+      (st = check_ranges(out, 4)) != DTP_OK)
     return st;
   if (T == 0) {
     if (dw0 && (st = fill_zeros(dw0, (int64_t)N * K, dtype, s)) != DTP_OK) return st;

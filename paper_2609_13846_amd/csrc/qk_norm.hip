@@ -361,10 +361,10 @@ dtp_status dtp_qk_norm_rotate_forward(int64_t n_tokens, int32_t n_q_heads, int32
                         {gamma_q, (size_t)es * dh, "gamma_q"}, {gamma_k, (size_t)es * dh, "gamma_k"},
                         {positions, sizeof(int32_t) * (size_t)T, "positions"},
                         {inv_freq, sizeof(float) * (size_t)(rot_dim / 2), "inv_freq"}};
-    const Range out[] = {{q_out, nq, "q_out", 16, q_stride == (int64_t)H * dh ? q : nullptr},
-                         {k_out, nk, "k_out", 16, k_stride == (int64_t)G * dh ? k : nullptr}};
-    if ((st = check_ranges(in, 6)) != DTP_OK || (st = check_ranges(out, 2)) != DTP_OK ||
-        (st = check_disjoint(out, 2, in, 6)) != DTP_OK)
+    const Range out[] = {{q_out, nq, "q_out", 16, q_stride == (int64_t)H * dh ? 0 : -1},
+                         {k_out, nk, "k_out", 16, k_stride == (int64_t)G * dh ? 1 : -1}};
+    if ((st = check_disjoint(out, 2, in, 6)) != DTP_OK || (st = check_ranges(in, 6)) != DTP_OK ||
+        (st = check_ranges(out, 2)) != DTP_OK)
       return st;
     p.q_out = q_out;
     p.k_out = k_out;
@@ -410,11 +410,11 @@ dtp_status dtp_qk_norm_rotate_backward(int64_t n_tokens, int32_t n_q_heads, int3
                         {some(positions), sizeof(int32_t) * (size_t)T, "positions"},
                         {some(inv_freq), sizeof(float) * (size_t)(rot_dim / 2), "inv_freq"},
                         {some(dq_out), nq, "dq_out"}, {some(dk_out), nk, "dk_out"}};
-    const Range out[] = {{some(dq), nq, "dq", 16, dq_out}, {some(dk), nk, "dk", 16, dk_out},
+    const Range out[] = {{some(dq), nq, "dq", 16, 6}, {some(dk), nk, "dk", 16, 7},
                          {dgamma_q, (size_t)es * dh, "dgamma_q"}, {dgamma_k, (size_t)es * dh, "dgamma_k"},
                          {workspace, (size_t)std::max<int64_t>(workspace_bytes, 0), "workspace"}};
-    if ((st = check_ranges(in, 8)) != DTP_OK || (st = check_ranges(out, 4)) != DTP_OK ||
-        (st = check_disjoint(out, 5, in, 8)) != DTP_OK)
+    if ((st = check_disjoint(out, 5, in, 8)) != DTP_OK || (st = check_ranges(in, 8)) != DTP_OK ||
+        (st = check_ranges(out, 4)) != DTP_OK)
       return st;
     if (T == 0) {
       if (dgamma_q == nullptr) return DTP_OK;

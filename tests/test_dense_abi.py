@@ -70,6 +70,32 @@ def test_host_memory_and_odd_addresses_are_refused():
         dtp.dtp_linear_forward(1, 8, 8, BF16, P, P, P, workspace=P)
 
 
+def overlaps(status, name):
+    return status == INVALID and dtp.lib().dtp_last_error().decode().endswith(name)
+
+
+def test_an_output_is_in_place_of_one_input_only():
+    """y may be the residual, but not where that is x too, which other blocks still read; so for the heads."""
+    lib, far = dtp.lib(), P + (1 << 16)
+    assert overlaps(lib.dtp_linear_forward(4, 8, 8, BF16, P, far, None, P, 0, 1.0, P, None, None, 0, None), "y overlaps x")
+    assert overlaps(lib.dtp_linear_forward(4, 8, 8, BF16, far, P, None, P, 0, 1.0, P, None, None, 0, None), "y overlaps w")
+    q, k, o, gamma, pos = (P + (i << 16) for i in range(5))
+
+    def forward(q, k, q_out, k_out):
+        return lib.dtp_qk_norm_rotate_forward(2, 2, 2, 64, BF16, q, 128, k, 128, gamma, gamma, 1e-6, pos, gamma, 64, q_out, k_out,
+                                              None)
+
+    def backward(dq_out, dk_out, dq, dk):
+        return lib.dtp_qk_norm_rotate_backward(2, 2, 2, 64, BF16, q, 128, k, 128, gamma, gamma, 1e-6, pos, gamma, 64, dq_out,
+                                               dk_out, dq, dk, None, None, None, 0, None)
+    assert overlaps(forward(q, q, q, o), "q_out overlaps k")
+    assert overlaps(forward(q, k, k, o), "q_out overlaps k")
+    assert overlaps(forward(k, k, o, k), "k_out overlaps q")
+    assert overlaps(backward(o, o, o, o + 512), "dq overlaps dk_out")
+    assert overlaps(backward(q, o, q, o + 512), "dq overlaps q")
+    assert overlaps(backward(o, o + 512, o + 1024, o), "dk overlaps dq_out")
+
+
 def test_workspace_sizes():
     """Enough for the backward pass is enough for the forward one; sizes do not shrink with it."""
     for T in (0, 1, 16, 100, 4096, 65536):
