@@ -425,7 +425,8 @@ int64_t dtp_qk_norm_rotate_workspace(int64_t n_tokens, int32_t n_q_heads, int32_
  *   gamma_q, gamma_k [dh], or both NULL: no norm
  *   positions [n_tokens] int32 and inv_freq [R/2] float, or both NULL with rot_dim R = 0: no
  *     rotation.  Angles are formed in 64 bits, so positions may be far, and of either sign.
- * head_dim even, 2 to 256; R even, at most head_dim; a norm, a rotation or both. */
+ * head_dim even, 2 to 256; H a multiple of G, at most 65,536; R even, at most head_dim; strides
+ * at most 2^32; a norm, a rotation or both. */
 dtp_status dtp_qk_norm_rotate_forward(int64_t n_tokens, int32_t n_q_heads, int32_t n_kv_groups,
                                       int32_t head_dim, dtp_dtype dtype, const void* q, int64_t q_stride,
                                       const void* k, int64_t k_stride, const void* gamma_q,

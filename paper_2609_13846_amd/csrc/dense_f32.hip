@@ -212,6 +212,11 @@ __global__ void __launch_bounds__(F > 1 ? 256 : 512, 2) tile_product_f32_kernel(
 // itself (in tiles of 128, whose four wavefronts leave the SIMDs one each).
 constexpr double kBig = 0.0158 * kStage, kSmall = 0.0195 * kStage, kBigAlone = 0.0190 * kStage, kSmallAlone = 0.0260 * kStage;
 
+// Tiles of 64 in a launch, of 512 threads each: a launch takes fewer than 2^32 threads, 2^23 of these
+// tiles.  (Tiles of 128, half the threads for twice the tokens, are few enough for any tensor that
+// fits a GPU.)
+constexpr int64_t kMostSmall = (int64_t)1 << 22;
+
 struct Shape {
   bool stream = false;
   int f = 2, splits = 1, per = 0, stages = 0, m_tiles = 0;
@@ -234,6 +239,7 @@ Shape choose(const Product& p) {
   for (int f = 1; f <= 2; ++f) {
     const int rows = gated ? 64 : 64 * f;
     const int64_t m_tiles = (p.M + rows - 1) / rows, n_tiles = (p.N + 64 * f - 1) / (64 * f);
+    if (f == 1 && m_tiles * n_tiles > kMostSmall) continue;
     const double sums = (gated ? 2.0 : f) * f;  // 64 x 64 of them in a tile
     for (int splits = 1; splits <= std::min(32, std::max(1, nq / 2)); ++splits) {
       const int per = (nq + splits - 1) / splits;

@@ -257,3 +257,16 @@ def test_far_offsets_of_heads():
     dtp.dtp_qk_norm_rotate_forward(T, H, G, dh, code, q, k, q, k, gamma_q=g, gamma_k=g, eps=EPS, positions=pos,
                                    inv_freq=frequencies(dh))
     ref.check(q[last], want, bound, "q")
+
+
+def test_more_tokens_than_a_launch_of_small_tiles_takes():
+    """2^29 fp32 tokens and some: 64 a tile and 512 threads would be 2^32 threads and more."""
+    T = 2 ** 29 + 70
+    announce("many tokens", T)
+    x = torch.arange(T, dtype=torch.int32, device="cuda").remainder_(1009).float()
+    w, y = torch.full((1, 1), 0.5, device="cuda"), torch.full((T,), -1.0, device="cuda")
+    space = workspace(dtp.dtp_linear_workspace(T, 1, 1, dtp.DTP_F32))
+    dtp.dtp_linear_forward(T, 1, 1, dtp.DTP_F32, x, w, y, workspace=space)
+    assert torch.equal(y, x.mul_(0.5))  # exact: halves of whole numbers
+    dtp.dtp_linear_backward(T, 1, 1, dtp.DTP_F32, None, w, y, dx=x)
+    assert torch.equal(x, y.mul_(0.5))
