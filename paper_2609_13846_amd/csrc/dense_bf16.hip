@@ -17,7 +17,6 @@ constexpr int kCus = 256;
 struct TileArgs {
   const uint16_t *a0, *a1, *b;
   RowContraction k;
-  int64_t K;          // columns of a segment
   int M, N, Mp;       // Mp: M rounded up to 8, the row of a partial sum
   int nq, per;        // stages (stream: runs of 64 columns) of the contraction, and of a split
   int m_tiles, n_tiles;
@@ -98,9 +97,9 @@ __device__ __forceinline__ void exchange_groups(u32x4& a, u32x4& b) {
   }
 }
 
-// One block per CU (256 x 256 tiles; two of 128 x 128, three of 128 x 64), each with a run of items: a tile, or a
-// split of its contraction.  Items are numbered so that the ones that run together on an XCD share
-// operands.
+// One block per CU (256 x 256 tiles; two of 128 x 128, three of 128 x 64), each with a run of items: a
+// tile, or a split of its contraction.  Items are numbered so that the ones that run together on an
+// XCD share operands.
 // ENDS: M need not be a multiple of 8.  (A kernel of its own for the linear epilogue, which has no
 // registers for the rows' ends beside the exchange of lines.)
 template <int AF, int BF, bool AT, bool BT, ProductKind KIND, bool ENDS>
@@ -303,9 +302,8 @@ struct Shape {
 
 // The tile and the splits of the contraction by the launch's estimated length in us: a CU's items, one
 // stage of 64 columns after the other, half of the operands' bytes at memory speed (the other half is
-// read beside the products), and the join of the parts.  Measured (T x K x N, the best of all tiles and splits against the choice): 64 x 14,336 x
-// 4,096 26.3, 26.3; 777 x 1,040 x 2,816 13.8, 13.8; dW of 16,384 x 4,096 x 1,536 184, 184 (128 x 128:
-// 234).
+// read beside the products), and the join of the parts.  The times per stage and item were fitted to
+// launches of every tile and split.
 struct Tile {
   int m, n;        // rows of A and of B
   int per_cu;      // blocks of a CU
@@ -315,8 +313,10 @@ struct Tile {
 constexpr Tile kTiles[] = {{256, 256, 1, 1.28, 1.32, 5.0}, {128, 128, 2, 0.50, 0.49, 1.0}, {128, 64, 3, 0.39, 0.33, 0.8}};
 
 // Up to 8 tokens the weights are streamed into registers, and up to 16 where they are few: each block
-// reads the tokens too, as many bytes as of weights at 16 tokens (14,336 x 4,096: 24 us for one token,
-// 31 for 16 and 27 in tiles; 4,096 x 4,096: 10 and 12.5).
+// reads the tokens too, as many bytes as of weights at 16 tokens.  14,336 x 4,096, streamed and in tiles:
+// 26.1 us and 29.9 for 8 tokens, 28.3 and 29.8 for 12, 30.9 and 29.9 for 16; 4,096 x 14,336: 31.5 and 27.4
+// for 12; 4,096 x 4,096: 9.0 and 12.4 for 8, 10.0 and 12.5 for 16; a gated block of 4,096 x 14,336: 48.1
+// and 48.7 for 8, 51.0 and 46.8 for 16.
 bool streams(const Product& p) {
   if (p.at || p.bt) return false;
   return p.N <= 8 || (p.N <= kStreamTokens && (int64_t)p.M * p.K <= ((int64_t)1 << 24));
@@ -425,7 +425,6 @@ dtp_status launch_product_bf16(const Product& p, char* workspace, hipStream_t s)
   t.a1 = padded(p.a1, la, workspace, s);
   t.b = padded(p.b, lb, workspace, s);
   DTP_HIP(hipGetLastError());
-  t.K = p.K;
   t.k.lda = (uint32_t)(la.pad ? pad32(la.n) : p.lda);
   t.k.ldb = (uint32_t)(lb.pad ? pad32(lb.n) : p.ldb);
   t.bytes_a = 2 * la.rows * (int64_t)t.k.lda;

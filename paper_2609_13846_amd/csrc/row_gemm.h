@@ -9,8 +9,10 @@
 //   across  an LDS line of all the rows per contraction index, its pairs of pieces exchanged by the
 //           line's number, and the fragments read with the transposing LDS read: 16 lanes take
 //           4 lines x 16 rows and each gets the 4 lines of its row.
-// Both read whole 128-byte lines of memory.  (Stages of 32 columns, 64 bytes of a row at a time, had
-// every line fetched twice from L2: 1,284 TFLOP/s for 8,192 x 4,096 x 28,672, both along.)
+// Both read whole 128-byte lines of memory, where stages of 32 columns would read half a line of a row
+// at a time.  8,192 x 4,096 x 28,672, both along: 1,384 TFLOP/s (a library product 1,577), the matrix
+// cores busy 72% of the time and the wavefronts at a wait for 43%; 65,536 x 1,024 x 6,144, with 16
+// stages a tile: 1,160 (1,133 when it ran at 1,414 without its writes).
 // Reads past the operand return zeros (the buffer's range for rows and lines behind the last, an
 // address out of range for the columns behind a row's last): sizes need not be whole tiles.
 //
@@ -28,8 +30,8 @@
 //   4  half 1, columns 32-63   reads the next stage's first fragments;  copies half 1 two stages on
 // so that every fragment is read a step before its products, a copy has five to seven steps to
 // land, and the copies, which a wavefront cannot pass while the path to L2 is busy, are shared out
-// (all between X and Y: 2 to 5% slower).  In a step the first product goes before the reads and
-// copies of its column (1 to 2%).  The stages of a block's items follow each other without a gap:
+// over the steps.  In a step the first product goes before the reads and copies of its column (0.6
+// to 3% over reads first; one read between any two products took the forward pass 1.4 times as long).  The stages of a block's items follow each other without a gap:
 // the copies run two stages ahead into the next item while the results of this one are written.
 #pragma once
 
