@@ -314,8 +314,8 @@ constexpr Tile kTiles[] = {{256, 256, 1, 1.28, 1.32, 5.0}, {128, 128, 2, 0.50, 0
 
 // Up to 8 tokens the weights are streamed into registers, and up to 16 where they are few: each block
 // reads the tokens too, as many bytes as of weights at 16 tokens.  14,336 x 4,096, streamed and in tiles:
-// 26.1 us and 29.9 for 8 tokens, 28.3 and 29.8 for 12, 30.9 and 29.9 for 16; 4,096 x 14,336: 31.5 and 27.4
-// for 12; 4,096 x 4,096: 9.0 and 12.4 for 8, 10.0 and 12.5 for 16; a gated block of 4,096 x 14,336: 48.1
+// 26.2 us and 27.1 for 8 tokens, 28.2 and 27.4 for 12, 31.4 and 28.0 for 16; 4,096 x 14,336: 31.7 and 27.5
+// for 12; 4,096 x 4,096: 8.8 and 11.1 for 8, 10.0 and 11.4 for 16; a gated block of 4,096 x 14,336: 48.1
 // and 48.7 for 8, 51.0 and 46.8 for 16.
 bool streams(const Product& p) {
   if (p.at || p.bt) return false;
