@@ -1,54 +1,16 @@
-// The products of a dense decoder layer (linear and gated operators): their description on the
-// host, and the activations and result writes that their kernels share (gfx950).
-//
-// Every product is  C[n][m] = sum_k A(m, k) B(n, k),  m contiguous in the results:
-//   forward   m output feature, n token,          k input feature   (A = W, B = x)
-//   dx        m input feature,  n token,          k output feature  (A = W transposed, B = dz)
-//   dW        m input feature,  n output feature, k token           (A = x, B = dz transposed)
+// The products of a dense decoder layer (linear and gated operators): their launches, and the
+// activations and result writes that their kernels share (gfx950).
 #pragma once
 
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
 
+#include "dense_plan.h"
 #include "dtp_internal.h"
 #include "tile_mfma.h"
 
 namespace dtp {
-
-enum ProductKind {
-  kProductLinear,  // y = residual + alpha act(C + bias), C + bias kept in `pre`
-  kProductGated,   // two products with one B: y = act(C0) C1, both kept in `pre`
-  kProductGrad,    // y = alpha C; rows n from n_split on go to y2
-};
-
-// Where an element (n, m) of a product goes, and what is done to it on the way.
-struct ProductOut {
-  void* y = nullptr;
-  void* y2 = nullptr;
-  const void* bias = nullptr;      // [M]
-  const void* residual = nullptr;  // [N][M]
-  float* pre = nullptr;            // linear [N][M], gated [N][2][M]
-  float alpha = 1.0f;
-  int act = DTP_ACT_NONE;
-  int64_t n_split = INT64_MAX;  // gradient rows: [0, n_keep) to y, n_split + [0, n_keep) to y2
-  int64_t n_keep = INT64_MAX;
-};
-
-struct Product {
-  ProductKind kind = kProductLinear;
-  int dtype = DTP_BF16;
-  const void* a0 = nullptr;  // a1: the up projection, or the second segment's matrix
-  const void* a1 = nullptr;
-  const void* b = nullptr;
-  int64_t lda = 0, ldb = 0;
-  bool at = false, bt = false;  // element (row, k) at [k * ld + row] instead of [row * ld + k]
-  int M = 0;
-  int64_t N = 0, K = 0;  // K per segment
-  int segments = 1;      // contraction over a0 and then, from column b_seg of B's rows on, over a1
-  int64_t b_seg = 0;
-  ProductOut out;
-};
 
 // ---- arguments of the dense operators (dense.hip)
 struct Range {  // a buffer of the caller's

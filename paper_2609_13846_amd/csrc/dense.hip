@@ -230,61 +230,10 @@ struct Plan {
 };
 
 size_t esize(int dtype) { return dtype == DTP_BF16 ? 2 : 4; }
-int pad32(int n) { return (n + 31) / 32 * 32; }
-
-Product forward_product(ProductKind kind, int64_t T, int K, int N, int dtype) {
-  Product p;
-  p.kind = kind;
-  p.dtype = dtype;
-  p.lda = p.ldb = K;
-  p.M = N;
-  p.N = T;
-  p.K = K;
-  return p;
-}
-
-// dx of n_parts stacked weight matrices: contraction over their rows.
-Product dx_product(int64_t T, int K, int N, int parts, int ld, int dtype) {
-  Product p;
-  p.kind = kProductGrad;
-  p.dtype = dtype;
-  p.at = true;
-  p.lda = K;
-  p.ldb = (int64_t)parts * ld;
-  p.M = K;
-  p.N = T;
-  p.K = N;
-  p.segments = parts;
-  p.b_seg = ld;
-  return p;
-}
-
-Product dw_product(int64_t T, int K, int N, int parts, int ld, int dtype) {
-  Product p;
-  p.kind = kProductGrad;
-  p.dtype = dtype;
-  p.at = p.bt = true;
-  p.lda = K;
-  p.ldb = (int64_t)parts * ld;
-  p.M = K;
-  p.N = parts == 1 ? N : (int64_t)parts * ld;
-  p.K = T;
-  if (parts > 1) {
-    p.out.n_split = ld;
-    p.out.n_keep = N;
-  }
-  return p;
-}
-
-// Whether dz is formed on its own: with an activation, and where the bf16 kernels cannot take dy's
-// rows in 16-byte pieces.
-bool needs_pass(int N, int dtype, bool gated, bool with_act) {
-  return gated || with_act || (dtype == DTP_BF16 && N % 8 != 0);
-}
 
 Plan backward_plan(int64_t T, int K, int N, int parts, int dtype, bool pass, bool sums) {
   Plan w;
-  w.ld = pass ? pad32(N) : N;
+  w.ld = pass ? (int)pad32(N) : N;
   size_t at = 0;
   if (pass) at = up256(esize(dtype) * (size_t)T * parts * w.ld);
   w.sums = at;

@@ -12,8 +12,6 @@
 namespace dtp {
 namespace {
 
-constexpr int kCus = 256;
-
 struct TileArgs {
   const uint16_t *a0, *a1, *b;
   RowContraction k;
@@ -293,73 +291,8 @@ __global__ void __launch_bounds__(256) pad_rows_kernel(const uint16_t* __restric
   }
 }
 
-// ---------------------------------------------------------------------------- plan
-struct Shape {
-  bool stream = false;
-  int tile = 0;        // of kTiles
-  int splits = 1, per = 0, nq = 0;
-};
-
-// The tile and the splits of the contraction by the launch's estimated length in us: a CU's items, one
-// stage of 64 columns after the other, half of the operands' bytes at memory speed (the other half is
-// read beside the products), and the join of the parts.  The times per stage and item were fitted to
-// launches of every tile and split.
-struct Tile {
-  int m, n;        // rows of A and of B
-  int per_cu;      // blocks of a CU
-  double alone, shared;  // us per stage: one item per CU, several
-  double item;     // us per item beside its stages: results, the first copies
-};
-constexpr Tile kTiles[] = {{256, 256, 1, 1.28, 1.32, 5.0}, {128, 128, 2, 0.50, 0.49, 1.0}, {128, 64, 3, 0.39, 0.33, 0.8}};
-
-// Up to 8 tokens the weights are streamed into registers, and up to 16 where they are few: each block
-// reads the tokens too, as many bytes as of weights at 16 tokens.  14,336 x 4,096, streamed and in tiles:
-// 26.2 us and 27.1 for 8 tokens, 28.2 and 27.4 for 12, 31.4 and 28.0 for 16; 4,096 x 14,336: 31.7 and 27.5
-// for 12; 4,096 x 4,096: 8.8 and 11.1 for 8, 10.0 and 11.4 for 16; a gated block of 4,096 x 14,336: 48.1
-// and 48.7 for 8, 51.0 and 46.8 for 16.
-bool streams(const Product& p) {
-  if (p.at || p.bt) return false;
-  return p.N <= 8 || (p.N <= kStreamTokens && (int64_t)p.M * p.K <= ((int64_t)1 << 24));
-}
-
-Shape choose(const Product& p) {
-  Shape s;
-  const bool gated = p.kind == kProductGated;
-  if (streams(p)) {
-    s.stream = true;
-    choose_stream<uint16_t>(p, s.nq, s.per);
-    s.splits = (s.nq + s.per - 1) / s.per;
-    return s;
-  }
-  // every item has an even number of stages
-  s.nq = (int)((p.K + 2 * kRowStage - 1) / (2 * kRowStage)) * 2 * p.segments;
-  const double M = (gated ? 2.0 : 1.0) * p.M, N = (double)p.N;
-  const double stream = 2.0 * (M + N) * (double)p.K * p.segments / 5.5e6;  // us at 5.5 TB/s
-  double best = 1e30;
-  for (int i = 0; i < 3; ++i) {
-    const Tile& t = kTiles[i];
-    const int64_t tiles = (((int64_t)M + t.m - 1) / t.m) * ((p.N + t.n - 1) / t.n);
-    for (int splits = 1; splits <= std::min(32, s.nq / 2); ++splits) {
-      const int per = (s.nq / 2 + splits - 1) / splits * 2;
-      const int real = (s.nq + per - 1) / per;
-      if (real != splits) continue;
-      const int64_t items = (tiles * splits + kCus - 1) / kCus;  // of a CU
-      double us = (double)items * (per * (items > 1 ? t.shared : t.alone) + t.item);
-      us += 0.5 * stream;
-      if (splits > 1) us += 3.0 + 8.0 * splits * M * N / 5e6;  // 32-bit parts written and read
-      if (us < best) {
-        best = us;
-        s.tile = i;
-        s.per = per;
-        s.splits = splits;
-      }
-    }
-  }
-  return s;
-}
-
+// ---------------------------------------------------------------------------- launches
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
-int64_t pad32(int64_t n) { return (n + 31) / 32 * 32; }
 
 // Rows and row length of an operand as it lies in memory.
 struct Lines {
@@ -367,10 +300,10 @@ struct Lines {
   bool pad;
   size_t bytes() const { return pad ? up256(2 * (size_t)(rows * pad32(n))) : 0; }
 };
-Lines lines_a(const Product& p) { return {p.at ? p.K : p.M, p.at ? p.M : p.K, p.lda % 8 != 0 && !streams(p)}; }
-Lines lines_b(const Product& p) { return {p.bt ? p.K : p.N, p.bt ? p.N : p.K, p.ldb % 8 != 0 && !streams(p)}; }
+Lines lines_a(const Product& p) { return {p.at ? p.K : p.M, p.at ? p.M : p.K, p.lda % 8 != 0 && !streams_bf16(p)}; }
+Lines lines_b(const Product& p) { return {p.bt ? p.K : p.N, p.bt ? p.N : p.K, p.ldb % 8 != 0 && !streams_bf16(p)}; }
 
-size_t partial_bytes(const Product& p, const Shape& s) {
+size_t partial_bytes(const Product& p, const ShapeBf16& s) {
   if (s.splits == 1) return 0;
   return sizeof(float) * (size_t)s.splits * (p.kind == kProductGated ? 2 : 1) * (size_t)p.N * ((p.M + 7) / 8 * 8);
 }
@@ -387,13 +320,13 @@ const uint16_t* padded(const void* in, const Lines& l, char*& at, hipStream_t s)
 }
 
 template <ProductKind KIND, bool AT, bool BT>
-void launch_tiles(TileArgs& t, const Shape& s, hipStream_t stream) {
+void launch_tiles(TileArgs& t, const ShapeBf16& s, hipStream_t stream) {
   if (KIND == kProductGated) {
     t.k.half_a = (const char*)t.a1 - (const char*)t.a0;
   } else {
-    t.k.half_a = t.k.half_left = (kTiles[s.tile].m / 2) * (AT ? 1 : (int64_t)t.k.lda);  // 8 AF rows
+    t.k.half_a = t.k.half_left = (kTilesBf16[s.tile].m / 2) * (AT ? 1 : (int64_t)t.k.lda);  // 8 AF rows
   }
-  const int items = t.m_tiles * t.n_tiles * s.splits, grid = std::min(items, kTiles[s.tile].per_cu * kCus);
+  const int items = t.m_tiles * t.n_tiles * s.splits, grid = std::min(items, kTilesBf16[s.tile].per_cu * kCus);
   auto launch = [&](auto ends) {
     constexpr bool kEnds = decltype(ends)::value;
     if (s.tile == 0)
@@ -414,11 +347,11 @@ void launch_tiles(TileArgs& t, const Shape& s, hipStream_t stream) {
 size_t product_bytes_bf16(const Product& p) {
   const Lines a = lines_a(p), b = lines_b(p);
   const bool two = p.kind == kProductGated || p.segments == 2;
-  return (two ? 2 : 1) * a.bytes() + b.bytes() + partial_bytes(p, choose(p));
+  return (two ? 2 : 1) * a.bytes() + b.bytes() + partial_bytes(p, choose_bf16(p));
 }
 
 dtp_status launch_product_bf16(const Product& p, char* workspace, hipStream_t s) {
-  const Shape shape = choose(p);
+  const ShapeBf16 shape = choose_bf16(p);
   const Lines la = lines_a(p), lb = lines_b(p);
   TileArgs t{};
   t.a0 = padded(p.a0, la, workspace, s);
@@ -449,8 +382,8 @@ dtp_status launch_product_bf16(const Product& p, char* workspace, hipStream_t s)
     StreamArgs r{t.a0, t.a1, t.b, t.k.lda, t.k.ldb, t.M, t.N, t.Mp, p.K, shape.nq, shape.per, shape.splits, t.partial, t.out};
     launch_stream<uint16_t>(p.kind, r, s);
   } else {
-    t.m_tiles = (int)(((int64_t)(p.kind == kProductGated ? 2 : 1) * p.M + kTiles[shape.tile].m - 1) / kTiles[shape.tile].m);
-    t.n_tiles = (int)((p.N + kTiles[shape.tile].n - 1) / kTiles[shape.tile].n);
+    t.m_tiles = (int)(((int64_t)(p.kind == kProductGated ? 2 : 1) * p.M + kTilesBf16[shape.tile].m - 1) / kTilesBf16[shape.tile].m);
+    t.n_tiles = (int)((p.N + kTilesBf16[shape.tile].n - 1) / kTilesBf16[shape.tile].n);
     switch (p.kind) {
       case kProductLinear: launch_tiles<kProductLinear, false, false>(t, shape, s); break;
       case kProductGated: launch_tiles<kProductGated, false, false>(t, shape, s); break;

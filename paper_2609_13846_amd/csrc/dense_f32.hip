@@ -15,8 +15,7 @@
 namespace dtp {
 namespace {
 
-constexpr int kCus = 256;
-constexpr int kStage = 32;             // columns per stage
+constexpr int kStage = kStageF32;      // columns per stage
 constexpr int kAlongRow = kStage + 4;  // floats: 16 rows' 16-byte reads cover the banks once
 
 typedef __attribute__((ext_vector_type(16))) float f32x16;
@@ -208,67 +207,14 @@ __global__ void __launch_bounds__(F > 1 ? 256 : 512, 2) tile_product_f32_kernel(
     }
 }
 
-// us of a CU per stage and 64 x 64 sums in tiles of 128 and of 64, and of an item that has the CU to
-// itself (in tiles of 128, whose four wavefronts leave the SIMDs one each).
-constexpr double kBig = 0.0158 * kStage, kSmall = 0.0195 * kStage, kBigAlone = 0.0190 * kStage, kSmallAlone = 0.0260 * kStage;
-
-// Tiles of 64 in a launch, of 512 threads each: a launch takes fewer than 2^32 threads, 2^23 of these
-// tiles.  (Tiles of 128, half the threads for twice the tokens, are few enough for any tensor that
-// fits a GPU.)
-constexpr int64_t kMostSmall = (int64_t)1 << 22;
-
-struct Shape {
-  bool stream = false;
-  int f = 2, splits = 1, per = 0, stages = 0, m_tiles = 0;
-  int64_t n_tiles = 0;
-};
-
-Shape choose(const Product& p) {
-  Shape s;
-  const bool gated = p.kind == kProductGated;
-  if (!p.at && !p.bt && p.N <= kStreamTokens) {
-    s.stream = true;
-    choose_stream<float>(p, s.stages, s.per);
-    s.splits = (s.stages + s.per - 1) / s.per;
-    return s;
-  }
-  s.stages = (int)((p.K + kStage - 1) / kStage);
-  const int nq = s.stages * p.segments;
-  const double planes = gated ? 2.0 : 1.0;
-  double best = 1e30;
-  for (int f = 1; f <= 2; ++f) {
-    const int rows = gated ? 64 : 64 * f;
-    const int64_t m_tiles = (p.M + rows - 1) / rows, n_tiles = (p.N + 64 * f - 1) / (64 * f);
-    if (f == 1 && m_tiles * n_tiles > kMostSmall) continue;
-    const double sums = (gated ? 2.0 : f) * f;  // 64 x 64 of them in a tile
-    for (int splits = 1; splits <= std::min(32, std::max(1, nq / 2)); ++splits) {
-      const int per = (nq + splits - 1) / splits;
-      if ((nq + per - 1) / per != splits) continue;
-      const int64_t items = (m_tiles * n_tiles * splits + kCus - 1) / kCus;  // of a CU
-      const double rate = items > 1 ? (f == 2 ? kBig : kSmall) : (f == 2 ? kBigAlone : kSmallAlone);
-      double us = (double)items * (per * sums * rate + 1.0);
-      if (splits > 1) us += 3.0 + 8.0 * splits * planes * p.M * (double)p.N / 5e6;  // parts written and read
-      if (us < best) {
-        best = us;
-        s.f = f;
-        s.m_tiles = (int)m_tiles;
-        s.n_tiles = n_tiles;
-        s.per = per;
-        s.splits = splits;
-      }
-    }
-  }
-  return s;
-}
-
-size_t partial_bytes(const Product& p, const Shape& s) {
+size_t partial_bytes(const Product& p, const ShapeF32& s) {
   return s.splits == 1 ? 0
                        : sizeof(float) * (size_t)s.splits * (p.kind == kProductGated ? 2 : 1) * (size_t)p.N *
                              (size_t)((p.M + 7) / 8 * 8);
 }
 
 template <ProductKind KIND, bool AT, bool BT>
-void launch_tiles(const TileArgs& t, const Shape& s, hipStream_t stream) {
+void launch_tiles(const TileArgs& t, const ShapeF32& s, hipStream_t stream) {
   const dim3 grid((unsigned)(s.m_tiles * s.n_tiles), s.splits);
   if (s.f == 2)
     tile_product_f32_kernel<2, AT, BT, KIND><<<grid, 256, 0, stream>>>(t);
@@ -278,10 +224,10 @@ void launch_tiles(const TileArgs& t, const Shape& s, hipStream_t stream) {
 
 }  // namespace
 
-size_t product_bytes_f32(const Product& p) { return partial_bytes(p, choose(p)); }
+size_t product_bytes_f32(const Product& p) { return partial_bytes(p, choose_f32(p)); }
 
 dtp_status launch_product_f32(const Product& p, char* workspace, hipStream_t s) {
-  const Shape shape = choose(p);
+  const ShapeF32 shape = choose_f32(p);
   const int Mp = (p.M + 7) / 8 * 8;
   float* partial = shape.splits > 1 ? (float*)workspace : nullptr;
   if (shape.stream) {

@@ -7,8 +7,6 @@
 
 namespace dtp {
 
-constexpr int kStreamTokens = 16;
-
 struct StreamArgs {
   const void *a0, *a1, *b;
   int64_t lda, ldb;
@@ -202,17 +200,6 @@ __global__ void __launch_bounds__(256) join_product_kernel(const float* __restri
       }
     write_product<S, KIND, W>(out, n, m, M, v[0], v[1]);
   }
-}
-
-// Runs of a few-token product, and how many a block takes: the contraction is split where the
-// features alone would leave CUs idle and every wavefront keeps at least four runs.
-template <typename S>
-void choose_stream(const Product& p, int& runs, int& per) {
-  runs = (int)((p.K * (int64_t)sizeof(S) + 127) / 128);
-  const int blocks = (p.M + 15) / 16;
-  int splits = 1;
-  while (blocks * splits < 128 && runs / (splits * 2) >= 32) splits *= 2;
-  per = (runs + splits - 1) / splits;
 }
 
 template <typename S, ProductKind KIND>

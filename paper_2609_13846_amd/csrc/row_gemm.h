@@ -39,13 +39,13 @@
 
 #include <cstdint>
 
+#include "dense_plan.h"
 #include "frag_gemm.h"
 
 namespace dtp {
 
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 
-constexpr int kRowStage = 64;                  // columns per stage
 constexpr uint32_t kRowRange = 0x80000000u;    // most bytes of an operand that a stage may reach
 constexpr uint32_t kOutOfRange = 0xc0000000u;  // an offset beyond any range
 

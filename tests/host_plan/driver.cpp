@@ -1,0 +1,44 @@
+// The launches that dense_plan.h chooses, from the header that the library's own calls use.  One
+// line in, "linear|gated tokens in out bf16|f32 act", gives one line per product out:
+//   forward|dx|dw  tile rows x columns (0 x 0: streamed)  splits  stages  stages per split  tiles
+#include <cstdio>
+#include <cstring>
+
+#include "dense_plan.h"
+
+using namespace dtp;
+
+static void print(const char* name, const Product& p, bool first) {
+  long long m, n, splits, stages, per, tiles;
+  const long long planes = p.kind == kProductGated ? 2 : 1;
+  bool stream;
+  if (p.dtype == DTP_BF16) {
+    const ShapeBf16 s = choose_bf16(p);
+    const Tile& t = kTilesBf16[s.tile];
+    stream = s.stream, splits = s.splits, stages = s.nq, per = s.per, m = t.m, n = t.n;
+    tiles = (planes * p.M + m - 1) / m * ((p.N + n - 1) / n);
+  } else {
+    const ShapeF32 s = choose_f32(p);
+    stream = s.stream, splits = s.splits, stages = (long long)s.stages * p.segments, per = s.per;
+    m = n = 64 * s.f;
+    tiles = (long long)s.m_tiles * s.n_tiles;
+  }
+  std::printf("%s%s %lld %lld %lld %lld %lld %lld", first ? "" : " ", name, stream ? 0 : m, stream ? 0 : n, splits, stages, per,
+              stream ? 0 : tiles);
+}
+
+int main() {
+  char kind[16], type[16];
+  long long T;
+  int K, N, act;
+  while (std::scanf("%15s %lld %d %d %15s %d", kind, &T, &K, &N, type, &act) == 6) {
+    const bool gated = !std::strcmp(kind, "gated");
+    const int dtype = !std::strcmp(type, "bf16") ? DTP_BF16 : DTP_F32, parts = gated ? 2 : 1;
+    const int ld = needs_pass(N, dtype, gated, act != DTP_ACT_NONE) ? (int)pad32(N) : N;
+    print("forward", forward_product(gated ? kProductGated : kProductLinear, T, K, N, dtype), true);
+    print("dx", dx_product(T, K, N, parts, ld, dtype), false);
+    print("dw", dw_product(T, K, N, parts, ld, dtype), false);
+    std::printf("\n");
+  }
+  return 0;
+}
