@@ -26,6 +26,7 @@ struct TileArgs {
   int M, Mp, segments;
   int64_t N;
   int m_tiles, per, stages;  // stages per split, and of a segment
+  uint32_t first;            // tile of the launch
   float* partial;
   ProductOut out;
 };
@@ -105,8 +106,8 @@ __global__ void __launch_bounds__(F > 1 ? 256 : 512, 2) tile_product_f32_kernel(
   __shared__ __attribute__((aligned(16))) float lds[2][kMats * SA::kFloats + SB::kFloats];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int wm = wave & 1, wn = wave >> 1 & 1, set = wave >> 2;
-  const int tm = blockIdx.x % p.m_tiles;
-  const int64_t m0 = (int64_t)tm * kRowsA, n0 = (int64_t)(blockIdx.x / p.m_tiles) * kTile;
+  const uint32_t tile = p.first + blockIdx.x;
+  const int64_t m0 = (int64_t)(tile % p.m_tiles) * kRowsA, n0 = (int64_t)(tile / p.m_tiles) * kTile;
   const int q0 = blockIdx.y * p.per, q1 = min(q0 + p.per, p.stages * p.segments);
   f32x16 acc[kMats][kFM][F] = {};
   struct {  // the stage on its way
@@ -214,12 +215,15 @@ size_t partial_bytes(const Product& p, const ShapeF32& s) {
 }
 
 template <ProductKind KIND, bool AT, bool BT>
-void launch_tiles(const TileArgs& t, const ShapeF32& s, hipStream_t stream) {
-  const dim3 grid((unsigned)(s.m_tiles * s.n_tiles), s.splits);
-  if (s.f == 2)
-    tile_product_f32_kernel<2, AT, BT, KIND><<<grid, 256, 0, stream>>>(t);
-  else
-    tile_product_f32_kernel<1, AT, BT, KIND><<<grid, 512, 0, stream>>>(t);
+void launch_tiles(TileArgs& t, const ShapeF32& s, hipStream_t stream) {
+  for (int64_t first = 0; first < s.m_tiles * s.n_tiles; first += kMostTilesF32) {
+    t.first = (uint32_t)first;  // of fewer than 2^32 tiles: their results are in memory
+    const dim3 grid((unsigned)s.launch_tiles(first), s.splits);
+    if (s.f == 2)
+      tile_product_f32_kernel<2, AT, BT, KIND><<<grid, s.threads(), 0, stream>>>(t);
+    else
+      tile_product_f32_kernel<1, AT, BT, KIND><<<grid, s.threads(), 0, stream>>>(t);
+  }
 }
 
 }  // namespace

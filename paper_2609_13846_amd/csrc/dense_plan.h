@@ -188,15 +188,17 @@ inline ShapeBf16 choose_bf16(const Product& p) {
 // itself (in tiles of 128, whose four wavefronts leave the SIMDs one each).
 constexpr double kBig = 0.0158 * kStageF32, kSmall = 0.0195 * kStageF32, kBigAlone = 0.0190 * kStageF32, kSmallAlone = 0.0260 * kStageF32;
 
-// Tiles of 64 in a launch, of 512 threads each: a launch takes fewer than 2^32 threads, 2^23 of these
-// tiles.  (Tiles of 128, half the threads for twice the tokens, are few enough for any tensor that
-// fits a GPU.)
-constexpr int64_t kMostSmall = (int64_t)1 << 22;
+// Tiles of one launch: a launch takes fewer than 2^32 threads, and a tile has at most 512.  More
+// tiles are more launches.
+constexpr int64_t kMostTilesF32 = (int64_t)1 << 22;
 
 struct ShapeF32 {
   bool stream = false;
   int f = 2, splits = 1, per = 0, stages = 0, m_tiles = 0;
   int64_t n_tiles = 0;
+  int threads() const { return f == 2 ? 256 : 512; }
+  // Tiles of the launch that starts with tile `first`.
+  int64_t launch_tiles(int64_t first) const { return std::min(m_tiles * n_tiles - first, kMostTilesF32); }
 };
 
 inline ShapeF32 choose_f32(const Product& p) {
@@ -215,7 +217,6 @@ inline ShapeF32 choose_f32(const Product& p) {
   for (int f = 1; f <= 2; ++f) {
     const int rows = gated ? 64 : 64 * f;
     const int64_t m_tiles = (p.M + rows - 1) / rows, n_tiles = (p.N + 64 * f - 1) / (64 * f);
-    if (f == 1 && m_tiles * n_tiles > kMostSmall) continue;
     const double sums = (gated ? 2.0 : f) * f;  // 64 x 64 of them in a tile
     for (int splits = 1; splits <= std::min(32, std::max(1, nq / 2)); ++splits) {
       const int per = (nq + splits - 1) / splits;

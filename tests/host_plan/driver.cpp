@@ -1,6 +1,7 @@
 // The launches that dense_plan.h chooses, from the header that the library's own calls use.  One
 // line in, "linear|gated tokens in out bf16|f32 act", gives one line per product out:
 //   forward|dx|dw  tile rows x columns (0 x 0: streamed)  splits  stages  stages per split  tiles
+//   threads of the largest launch, along its longest axis
 #include <cstdio>
 #include <cstring>
 
@@ -9,7 +10,7 @@
 using namespace dtp;
 
 static void print(const char* name, const Product& p, bool first) {
-  long long m, n, splits, stages, per, tiles;
+  long long m, n, splits, stages, per, tiles, threads;
   const long long planes = p.kind == kProductGated ? 2 : 1;
   bool stream;
   if (p.dtype == DTP_BF16) {
@@ -17,14 +18,16 @@ static void print(const char* name, const Product& p, bool first) {
     const Tile& t = kTilesBf16[s.tile];
     stream = s.stream, splits = s.splits, stages = s.nq, per = s.per, m = t.m, n = t.n;
     tiles = (planes * p.M + m - 1) / m * ((p.N + n - 1) / n);
+    threads = (tiles * splits < t.per_cu * kCus ? tiles * splits : t.per_cu * kCus) * 512;
   } else {
     const ShapeF32 s = choose_f32(p);
     stream = s.stream, splits = s.splits, stages = (long long)s.stages * p.segments, per = s.per;
     m = n = 64 * s.f;
     tiles = (long long)s.m_tiles * s.n_tiles;
+    threads = stream ? 0 : (long long)s.launch_tiles(0) * s.threads();
   }
-  std::printf("%s%s %lld %lld %lld %lld %lld %lld", first ? "" : " ", name, stream ? 0 : m, stream ? 0 : n, splits, stages, per,
-              stream ? 0 : tiles);
+  if (stream) m = n = tiles = 0, threads = (p.M + 15) / 16 * 512;
+  std::printf("%s%s %lld %lld %lld %lld %lld %lld %lld", first ? "" : " ", name, m, n, splits, stages, per, tiles, threads);
 }
 
 int main() {

@@ -34,8 +34,8 @@ def plans(tmp_path_factory):
         out = []
         for line in run.stdout.splitlines():
             f = line.split()
-            out.append({f[i]: dict(zip(("m", "n", "splits", "stages", "per", "tiles"), map(int, f[i + 1:i + 7])))
-                        for i in range(0, len(f), 7)})
+            out.append({f[i]: dict(zip(("m", "n", "splits", "stages", "per", "tiles", "threads"), map(int, f[i + 1:i + 8])))
+                        for i in range(0, len(f), 8)})
         assert len(out) == len(lines)
         return out
 
@@ -80,3 +80,12 @@ def test_splits_cover_the_contraction(plans):
             assert (p["splits"] - 1) * p["per"] < p["stages"] <= p["splits"] * p["per"], (line, name, p)
             if p["m"] and line[4] == "bf16":
                 assert p["per"] % 2 == 0 and p["stages"] % 2 == 0, (line, name, p)
+
+
+def test_launches_have_fewer_than_2_to_the_32_threads(plans):
+    """Of the longest and narrowest tensors that are taken, whose results still fit the GPU."""
+    lines = [(kind, T, K, N, dtype, 1) for kind in ("linear", "gated") for dtype in ("bf16", "f32")
+             for T in (1 << 28, (1 << 29) + 70, (1 << 30) - 1, 1 << 30) for K, N in ((1, 1), (1, 64), (1, 65), (65, 1), (1, 129))]
+    for line, got in zip(lines, plans(lines)):
+        for name, p in got.items():
+            assert 0 < p["threads"] < 2 ** 32, (line, name, p)

@@ -81,3 +81,15 @@ def test_gated(dtype, T, I):
     dtp.dtp_gated_backward(T, K, I, code, x, wg, wu, pre, dh, dx=dx, dw_gate=dwg, dw_up=dwu, workspace=space)
     assert torch.equal(dwg, product(dg.t(), x[at].t()).to(dt)) and torch.equal(dwu, product(du.t(), x[at].t()).to(dt))
     assert torch.equal(dx[at], (product(dg, wg.t()) + product(du, wu.t())).to(dt)) and zero_elsewhere(dx, at)
+
+
+def test_more_tiles_than_a_launch_takes():
+    """2^28 fp32 tokens and some through 65 neurons: more than 2^22 tiles of 128 tokens x 64 neurons.
+    x of 0 or 128, where silu is x exactly: h = 128 (128 w_up)."""
+    T, I = 2 ** 28 + 70, 65
+    print("[gpu] many tiles", T, I, file=sys.stderr, flush=True)
+    x = torch.arange(T, dtype=torch.int32, device="cuda").remainder_(3).clamp_(max=1).float().mul_(128).view(T, 1)
+    wg, wu = torch.ones(I, 1, device="cuda"), whole(1, 8, I, 1)
+    h = torch.full((T, I), -1.0, device="cuda")
+    dtp.dtp_gated_forward(T, 1, I, dtp.DTP_F32, x, wg, wu, h)
+    assert all(torch.equal(a, b * (128 * wu.view(1, I))) for a, b in zip(h.split(1 << 22), x.split(1 << 22)))
