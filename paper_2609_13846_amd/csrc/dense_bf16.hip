@@ -326,7 +326,7 @@ void launch_tiles(TileArgs& t, const ShapeBf16& s, hipStream_t stream) {
   } else {
     t.k.half_a = t.k.half_left = (kTilesBf16[s.tile].m / 2) * (AT ? 1 : (int64_t)t.k.lda);  // 8 AF rows
   }
-  const int items = t.m_tiles * t.n_tiles * s.splits, grid = std::min(items, kTilesBf16[s.tile].per_cu * kCus);
+  const int items = t.m_tiles * t.n_tiles * s.splits, grid = std::min(items, kTilesBf16[s.tile].per_cu * device_cus());
   auto launch = [&](auto ends) {
     constexpr bool kEnds = decltype(ends)::value;
     if (s.tile == 0)
@@ -347,11 +347,11 @@ void launch_tiles(TileArgs& t, const ShapeBf16& s, hipStream_t stream) {
 size_t product_bytes_bf16(const Product& p) {
   const Lines a = lines_a(p), b = lines_b(p);
   const bool two = p.kind == kProductGated || p.segments == 2;
-  return (two ? 2 : 1) * a.bytes() + b.bytes() + partial_bytes(p, choose_bf16(p));
+  return (two ? 2 : 1) * a.bytes() + b.bytes() + partial_bytes(p, choose_bf16(p, device_cus()));
 }
 
 dtp_status launch_product_bf16(const Product& p, char* workspace, hipStream_t s) {
-  const ShapeBf16 shape = choose_bf16(p);
+  const ShapeBf16 shape = choose_bf16(p, device_cus());
   const Lines la = lines_a(p), lb = lines_b(p);
   TileArgs t{};
   t.a0 = padded(p.a0, la, workspace, s);

@@ -228,10 +228,10 @@ void launch_tiles(TileArgs& t, const ShapeF32& s, hipStream_t stream) {
 
 }  // namespace
 
-size_t product_bytes_f32(const Product& p) { return partial_bytes(p, choose_f32(p)); }
+size_t product_bytes_f32(const Product& p) { return partial_bytes(p, choose_f32(p, device_cus())); }
 
 dtp_status launch_product_f32(const Product& p, char* workspace, hipStream_t s) {
-  const ShapeF32 shape = choose_f32(p);
+  const ShapeF32 shape = choose_f32(p, device_cus());
   const int Mp = (p.M + 7) / 8 * 8;
   float* partial = shape.splits > 1 ? (float*)workspace : nullptr;
   if (shape.stream) {

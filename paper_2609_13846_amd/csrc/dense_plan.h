@@ -15,7 +15,6 @@
 
 namespace dtp {
 
-constexpr int kCus = 256;
 constexpr int kRowStage = 64;  // columns per stage: bf16 tiles
 constexpr int kStageF32 = 32;  // fp32 tiles
 constexpr int kStreamTokens = 16;
@@ -107,14 +106,14 @@ inline bool needs_pass(int N, int dtype, bool gated, bool with_act) {
   return gated || with_act || (dtype == DTP_BF16 && N % 8 != 0);
 }
 
-// ---- their launches
+// ---- their launches, on a GPU of `cus` compute units
 // Runs of a few-token product, and how many a block takes: the contraction is split where the
-// features alone would leave CUs idle and every wavefront keeps at least four runs.
-inline void choose_stream(const Product& p, int64_t es, int& runs, int& per) {
+// features alone would leave half of the CUs idle and every wavefront keeps at least four runs.
+inline void choose_stream(const Product& p, int cus, int64_t es, int& runs, int& per) {
   runs = (int)((p.K * es + 127) / 128);
   const int blocks = (p.M + 15) / 16;
   int splits = 1;
-  while (blocks * splits < 128 && runs / (splits * 2) >= 32) splits *= 2;
+  while (blocks * splits < cus / 2 && runs / (splits * 2) >= 32) splits *= 2;
   per = (runs + splits - 1) / splits;
 }
 
@@ -147,12 +146,12 @@ inline bool streams_bf16(const Product& p) {
   return p.N <= 8 || (p.N <= kStreamTokens && (int64_t)p.M * p.K <= ((int64_t)1 << 24));
 }
 
-inline ShapeBf16 choose_bf16(const Product& p) {
+inline ShapeBf16 choose_bf16(const Product& p, int cus) {
   ShapeBf16 s;
   const bool gated = p.kind == kProductGated;
   if (streams_bf16(p)) {
     s.stream = true;
-    choose_stream(p, 2, s.nq, s.per);
+    choose_stream(p, cus, 2, s.nq, s.per);
     s.splits = (s.nq + s.per - 1) / s.per;
     return s;
   }
@@ -168,7 +167,7 @@ inline ShapeBf16 choose_bf16(const Product& p) {
       const int per = (s.nq / 2 + splits - 1) / splits * 2;
       const int real = (s.nq + per - 1) / per;
       if (real != splits) continue;
-      const int64_t items = (tiles * splits + kCus - 1) / kCus;  // of a CU
+      const int64_t items = (tiles * splits + cus - 1) / cus;  // of a CU
       double us = (double)items * (per * (items > 1 ? t.shared : t.alone) + t.item);
       us += 0.5 * stream;
       if (splits > 1) us += 3.0 + 8.0 * splits * M * N / 5e6;  // 32-bit parts written and read
@@ -201,12 +200,12 @@ struct ShapeF32 {
   int64_t launch_tiles(int64_t first) const { return std::min(m_tiles * n_tiles - first, kMostTilesF32); }
 };
 
-inline ShapeF32 choose_f32(const Product& p) {
+inline ShapeF32 choose_f32(const Product& p, int cus) {
   ShapeF32 s;
   const bool gated = p.kind == kProductGated;
   if (!p.at && !p.bt && p.N <= kStreamTokens) {
     s.stream = true;
-    choose_stream(p, 4, s.stages, s.per);
+    choose_stream(p, cus, 4, s.stages, s.per);
     s.splits = (s.stages + s.per - 1) / s.per;
     return s;
   }
@@ -221,7 +220,7 @@ inline ShapeF32 choose_f32(const Product& p) {
     for (int splits = 1; splits <= std::min(32, std::max(1, nq / 2)); ++splits) {
       const int per = (nq + splits - 1) / splits;
       if ((nq + per - 1) / per != splits) continue;
-      const int64_t items = (m_tiles * n_tiles * splits + kCus - 1) / kCus;  // of a CU
+      const int64_t items = (m_tiles * n_tiles * splits + cus - 1) / cus;  // of a CU
       const double rate = items > 1 ? (f == 2 ? kBig : kSmall) : (f == 2 ? kBigAlone : kSmallAlone);
       double us = (double)items * (per * sums * rate + 1.0);
       if (splits > 1) us += 3.0 + 8.0 * splits * planes * p.M * (double)p.N / 5e6;  // parts written and read

@@ -2,6 +2,7 @@
 // line in, "linear|gated tokens in out bf16|f32 act", gives one line per product out:
 //   forward|dx|dw  tile rows x columns (0 x 0: streamed)  splits  stages  stages per split  tiles
 //   threads of the largest launch, along its longest axis
+// The argument: compute units of the GPU, 256 without it.
 #include <cstdio>
 #include <cstring>
 
@@ -9,18 +10,20 @@
 
 using namespace dtp;
 
+static int cus = 256;
+
 static void print(const char* name, const Product& p, bool first) {
   long long m, n, splits, stages, per, tiles, threads;
   const long long planes = p.kind == kProductGated ? 2 : 1;
   bool stream;
   if (p.dtype == DTP_BF16) {
-    const ShapeBf16 s = choose_bf16(p);
+    const ShapeBf16 s = choose_bf16(p, cus);
     const Tile& t = kTilesBf16[s.tile];
     stream = s.stream, splits = s.splits, stages = s.nq, per = s.per, m = t.m, n = t.n;
     tiles = (planes * p.M + m - 1) / m * ((p.N + n - 1) / n);
-    threads = (tiles * splits < t.per_cu * kCus ? tiles * splits : t.per_cu * kCus) * 512;
+    threads = (tiles * splits < t.per_cu * cus ? tiles * splits : t.per_cu * cus) * 512;
   } else {
-    const ShapeF32 s = choose_f32(p);
+    const ShapeF32 s = choose_f32(p, cus);
     stream = s.stream, splits = s.splits, stages = (long long)s.stages * p.segments, per = s.per;
     m = n = 64 * s.f;
     tiles = (long long)s.m_tiles * s.n_tiles;
@@ -30,7 +33,8 @@ static void print(const char* name, const Product& p, bool first) {
   std::printf("%s%s %lld %lld %lld %lld %lld %lld %lld", first ? "" : " ", name, m, n, splits, stages, per, tiles, threads);
 }
 
-int main() {
+int main(int argc, char** argv) {
+  if (argc > 1) std::sscanf(argv[1], "%d", &cus);
   char kind[16], type[16];
   long long T;
   int K, N, act;

@@ -26,10 +26,10 @@ def plans(tmp_path_factory):
                            capture_output=True, text=True, timeout=300)
     assert build.returncode == 0, build.stderr[-4000:]
 
-    def ask(lines):
+    def ask(lines, cus=256):
         """For each (kind, tokens, in, out, dtype, act): {product: {"m", "n", "splits", ..}}."""
         text = "\n".join(" ".join(map(str, line)) for line in lines) + "\n"
-        run = subprocess.run([str(exe)], input=text, capture_output=True, text=True, timeout=300)
+        run = subprocess.run([str(exe), str(cus)], input=text, capture_output=True, text=True, timeout=300)
         assert run.returncode == 0, run.stderr[-4000:]
         out = []
         for line in run.stdout.splitlines():
@@ -89,3 +89,14 @@ def test_launches_have_fewer_than_2_to_the_32_threads(plans):
     for line, got in zip(lines, plans(lines)):
         for name, p in got.items():
             assert 0 < p["threads"] < 2 ** 32, (line, name, p)
+
+
+def test_plans_follow_the_compute_units(plans):
+    """A part of the GPU gets no more blocks than it holds at a time, and splits the contraction for no
+    more than it has; what fills the whole GPU is split on neither."""
+    few, some, many = ("linear", 16, 14336, 4096, "bf16", 0), ("linear", 400, 4096, 1024, "f32", 0), ("gated", 8192, 4096, 14336, "bf16", 1)
+    whole, part = plans([few, some, many]), plans([few, some, many], 32)
+    for w, p in zip(whole[:2], part):
+        assert w["forward"]["splits"] > p["forward"]["splits"]
+    for cus, g in ((256, whole[2]), (32, part[2])):
+        assert g["forward"]["splits"] == 1 and g["forward"]["m"] == 256 and g["forward"]["threads"] == 512 * cus
