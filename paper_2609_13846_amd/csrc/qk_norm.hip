@@ -74,7 +74,8 @@ __device__ __forceinline__ void store_piece(S* p, const float (&v)[V]) {
   *reinterpret_cast<Piece*>(p) = x;
 }
 
-__device__ __forceinline__ float head_sum(float v, int lanes) {
+template <typename F>
+__device__ __forceinline__ F head_sum(F v, int lanes) {
   for (int d = 1; d < lanes; d *= 2) v += __shfl_xor(v, d);
   return v;
 }
@@ -129,7 +130,19 @@ __global__ void __launch_bounds__(256) qk_kernel(QkArgs p) {
         for (int s = 0; s < NS; ++s)
 #pragma unroll
           for (int i = 0; i < V; ++i) sq = fmaf(v[s][0][i], v[s][0][i], fmaf(v[s][1][i], v[s][1][i], sq));
-        inv = 1.0f / sqrtf(head_sum(sq, p.lanes) / (float)p.dh + p.eps);
+        const float r2 = head_sum(sq, p.lanes) / (float)p.dh + p.eps;
+        if (r2 > 0x1p-100f && r2 < INFINITY) {
+          inv = 1.0f / sqrtf(r2);
+        } else {  // squares outside the range of 32 bits (or zeros, or not finite); all of a head's lanes
+          double wide = 0.0;
+#pragma unroll
+          for (int s = 0; s < NS; ++s)
+#pragma unroll
+            for (int i = 0; i < V; ++i) wide += (double)v[s][0][i] * v[s][0][i] + (double)v[s][1][i] * v[s][1][i];
+          wide = fma((double)p.dh, (double)p.eps, head_sum(wide, p.lanes));
+          const int e = __builtin_amdgcn_frexp_exp(wide) & ~1;
+          inv = ldexpf(1.0f / sqrtf((float)ldexp(wide, -e) / (float)p.dh), -e / 2);
+        }
         if (!in) inv = 0.0f;  // no head: nothing for dgamma, whatever eps
       }
       if constexpr (!BACKWARD) {
