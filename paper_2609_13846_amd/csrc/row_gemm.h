@@ -8,7 +8,11 @@
 //           row's number, so that the 16 rows of a fragment lie in different banks;
 //   across  an LDS line of all the rows per contraction index, its pairs of pieces exchanged by the
 //           line's number, and the fragments read with the transposing LDS read: 16 lanes take
-//           4 lines x 16 rows and each gets the 4 lines of its row.
+//           4 lines x 16 rows and each gets the 4 lines of its row.  A wavefront's read of B takes
+//           each bank twice, the least that its 512 bytes can; one of A takes half of the banks
+//           four times, since A's rows are dealt (below) so that it reads the lower or the upper
+//           halves of its pieces, which no exchange of whole pieces spreads: 40% of the LDS
+//           cycles of dx and dW are conflicts.
 // Both read whole 128-byte lines of memory, where stages of 32 columns would read half a line of a row
 // at a time.  8,192 x 4,096 x 28,672, both along: 1,384 TFLOP/s (a library product 1,577), the matrix
 // cores busy 72% of the time and the wavefronts at a wait for 43%; 65,536 x 1,024 x 6,144, with 16
@@ -49,8 +53,8 @@ typedef __attribute__((ext_vector_type(4))) short s16x4;
 constexpr uint32_t kRowRange = 0x80000000u;    // most bytes of an operand that a stage may reach
 constexpr uint32_t kOutOfRange = 0xc0000000u;  // an offset beyond any range
 
-// Exchange of an across-line's pairs of pieces, so that the lines 8 g + 0 .. 3 of all g, which one
-// transposing read of a wavefront takes, lie in different banks.
+// Exchange of an across-line's pairs of pieces by the lines 8 g + 0 .. 3 of all g, which one
+// transposing read of a wavefront takes: their pairs lie in different banks.
 template <int ROWS>
 __device__ __forceinline__ int across_swizzle(int line) {
   if constexpr (ROWS == 256) return (line & 3) | ((line >> 3) & 3) << 2;
