@@ -2,8 +2,8 @@
 contraction, with one item a block and several, at widths that are and are not multiples of 8.
 
 A case: kind, dtype, tokens, inputs, outputs, and what the launches are: for the forward product, dx
-and dW the tile's rows, "whole" or "split", and "many" where a block has several items (bf16; a
-tile of 256 has a compute unit to itself).  tests/test_dense_plan.py holds the library's choice to
+and dW the tile's columns (256, 128, and for bf16 64 of 128 x 64), "whole" or "split", and "many"
+where a block has several items (bf16; a tile of 256 has a compute unit to itself).  tests/test_dense_plan.py holds the library's choice to
 these on the host, tests/test_gpu_dense_tiles.py runs them.
 """
 
@@ -43,6 +43,24 @@ CASES = [
     ("gated", "bf16", 12352, 272, 6285, dict(forward=(256, W, "many"), dx=(256, S, "many"), dw=(256, S, ""))),
     ("gated", "bf16", 256, 3528, 3544, dict(dw=(256, W, "many"))),
     ("gated", "bf16", 256, 3503, 3576, dict(dw=(256, W, "many"))),
+    # bf16 blocks of several items in the smaller tiles
+    ("linear", "bf16", 1040, 132, 7480, dict(forward=(64, W, "many"))),
+    ("linear", "bf16", 4672, 178, 1703, dict(forward=(64, W, "many"))),
+    ("gated", "bf16", 408, 129, 8296, dict(forward=(64, W, "many"))),
+    ("gated", "bf16", 782, 176, 4747, dict(forward=(64, W, "many"))),
+    ("gated", "bf16", 16, 7816, 8432, dict(forward=(64, S, "many"))),
+    ("linear", "bf16", 1466, 5623, 144, dict(dx=(64, W, "many"))),
+    ("linear", "bf16", 8352, 931, 134, dict(dx=(128, W, "many"))),
+    ("linear", "bf16", 16640, 64, 8256, dict(dx=(128, S, "many"))),
+    ("linear", "bf16", 168, 8556, 931, dict(dw=(64, W, "many"))),
+    ("linear", "bf16", 136, 8033, 1032, dict(dw=(128, W, "many"))),
+    ("linear", "bf16", 19600, 1, 6650, dict(dw=(128, S, "many"))),
+    ("gated", "bf16", 2210, 3665, 64, dict(dx=(64, W, "many"))),
+    ("gated", "bf16", 18848, 449, 1, dict(dx=(128, W, "many"))),
+    ("gated", "bf16", 17952, 64, 4480, dict(dx=(128, S, "many"))),
+    ("gated", "bf16", 192, 2380, 1672, dict(dw=(64, W, "many"))),
+    ("gated", "bf16", 136, 1017, 4144, dict(dw=(128, W, "many"))),
+    ("gated", "bf16", 3200, 1, 8791, dict(dw=(128, S, "many"))),
     # fp32 tiles of 128 (those of 64 are every small call's)
     ("linear", "f32", 4320, 104, 728, dict(forward=(128, W, ""))),
     ("linear", "f32", 1360, 112, 2253, dict(forward=(128, W, ""))),

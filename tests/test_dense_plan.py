@@ -11,7 +11,7 @@ from paper_2609_13846_amd import dtp
 from tests.dense_tiles import CASES
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
-PER_CU = {256: 1, 128: 2}  # bf16 blocks of a compute unit
+PER_CU = {256: 1, 128: 2, 64: 3}  # bf16 blocks of a compute unit
 
 
 @pytest.fixture(scope="module")
@@ -46,29 +46,31 @@ def test_sizes_take_the_tiles_that_they_are_listed_for(plans):
     got = plans([(kind, T, K, N, dtype, dtp.DTP_ACT_SILU if kind == "gated" else dtp.DTP_ACT_NONE)
                  for kind, dtype, T, K, N, _ in CASES])
     for (kind, dtype, T, K, N, want), g in zip(CASES, got):
-        for name, (rows, parts, many) in want.items():
+        for name, (cols, parts, many) in want.items():
             p = g[name]
             case = (kind, dtype, T, K, N, name, p)
-            assert p["m"] == p["n"] == rows, case
+            assert p["n"] == cols and p["m"] == max(cols, 128), case
             assert (p["splits"] > 1) == (parts == "split"), case
             assert p["stages"] >= 3, case
             if many:
-                assert p["tiles"] * p["splits"] > 256 * PER_CU[rows], case
+                assert p["tiles"] * p["splits"] > 256 * PER_CU[cols], case
 
 
 def test_every_kernel_of_large_tiles_is_listed():
     """Kind, dtype, product, tile and splitting; for bf16 forward rows, whether they end inside a piece of eight."""
-    def reached(kind, dtype, name, rows, parts, odd=None):
-        return any(c[0] == kind and c[1] == dtype and c[5].get(name, (0, ""))[:2] == (rows, parts) and
-                   (odd is None or (c[4] % 8 != 0) == odd) for c in CASES)
+    def reached(kind, dtype, name, cols, parts, odd=None, many=""):
+        return any(c[0] == kind and c[1] == dtype and c[5].get(name, (0, ""))[:2] == (cols, parts) and
+                   many in c[5][name][2] and (odd is None or (c[4] % 8 != 0) == odd) for c in CASES)
     for kind in ("linear", "gated"):
-        for dtype, rows in (("bf16", 256), ("f32", 128)):
+        for dtype, cols in (("bf16", 256), ("f32", 128)):
             for name in ("forward", "dx", "dw"):
                 for parts in ("whole", "split"):
-                    assert reached(kind, dtype, name, rows, parts), (kind, dtype, name, parts)
-        for rows in (128, 256):
+                    assert reached(kind, dtype, name, cols, parts), (kind, dtype, name, parts)
+        for cols in (64, 128, 256):
             for odd in (False, True):
-                assert reached(kind, "bf16", "forward", rows, "whole", odd), (kind, rows, odd)
+                assert reached(kind, "bf16", "forward", cols, "whole", odd, "many"), (kind, cols, odd)
+            for name in ("dx", "dw"):
+                assert cols == 256 or reached(kind, "bf16", name, cols, "whole", many="many"), (kind, cols, name)
 
 
 def test_splits_cover_the_contraction(plans):
