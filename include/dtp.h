@@ -347,11 +347,11 @@ dtp_status dtp_apply_layout(const dtp_layer_desc* desc, int32_t L, const int32_t
  *     the way.  Results are deterministic for fixed shapes.
  *   - Outputs must not overlap inputs or each other, except where said (DTP_ERR_INVALID_ARG).
  *   - `workspace` (dev, `workspace_bytes` long, or NULL) is scratch of at least the size that
- *     the operator's _workspace function gives on the same device; it holds nothing between calls, and calls that
- *     share it must be ordered (one stream, or synchronised; so must replays of graphs that
- *     captured it).  With a workspace a call makes no allocation and can be captured into a
- *     graph.  With NULL the scratch comes from the stream-ordered allocator, which is refused
- *     under capture (DTP_ERR_UNSUPPORTED) where a call needs any.
+ *     the operator's _workspace function gives on the same device; it holds nothing between
+ *     calls, and calls that share it must be ordered (one stream, or synchronised; so must
+ *     replays of graphs that captured it).  With a workspace a call makes no allocation and can
+ *     be captured into a graph.  With NULL the scratch comes from the stream-ordered allocator,
+ *     which is refused under capture (DTP_ERR_UNSUPPORTED) where a call needs any.
  * ------------------------------------------------------------------------------------- */
 
 /* Activations: none, silu(z) = z / (1 + e^-z), gelu(z) = z/2 (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))). */
